@@ -10,6 +10,8 @@
  * The four entry points a caller of the method needs are attn_fwd, attn_fwd_launch_info, attn_last_error
  * and attn_version.  The others serve the studies of the paper's Sec. 3 and Sec. 4.3 (launch variants,
  * recorded schedules), bfloat16 inputs with caller-provided or built-in scratch memory, and older names.
+ * attn_kv_pages, attn_qkv_prepare and attn_decode carry on after the prompt: one new token per request over a
+ * paged key-value cache.
  */
 #ifndef SAWATTN_H
 #define SAWATTN_H
@@ -292,6 +294,131 @@ int attn_fwd_variant_launch_info(int B, int H, int N, int d, int causal, int in_
  */
 int attn_fwd_plan(int B, int H, int N, int d, int causal, int scan_order, int in_dtype,
                   const sawattn_variant* variant, int32_t* trace, int32_t* trace_count);
+
+/*
+ * Decoding over a paged key-value cache.  After the prompt, which attn_fwd computes, a serving program adds one token (or a
+ * few) per request and step: attn_kv_pages gives the new tokens cache slots, attn_qkv_prepare normalises and rotates
+ * their queries and keys and writes keys and values to those slots, attn_decode computes the attention of each request's
+ * newest token over everything the cache holds of it.  All three read lengths, tables and slots on the device, so that
+ * a step captured into a HIP graph stays right as the requests grow.
+ *
+ * A cache is cut into pages of `page_size` rows; row j of a request's keys is row j % page_size of page
+ * table[request][j / page_size].  A slot is the number page * page_size + row.
+ */
+typedef struct sawattn_kv_cache {
+    void* k;                 /* device.  Element e of row i of head h of page p: k[p*k_page + h*k_head + i*k_row + e] */
+    void* v;                 /* device.  The same with the strides of v */
+    int64_t k_page, k_head, k_row;      /* strides in elements: not negative, multiples of 8 */
+    int64_t v_page, v_head, v_row;
+    int pages;               /* >= 1 */
+    int page_size;           /* rows per page: a power of two, 8..2^20 */
+    int heads;               /* key/value heads, >= 1 */
+    int d;                   /* head dimension, 64 or 128; its elements lie side by side */
+    int dtype;               /* SAWATTN_F16 or SAWATTN_BF16 */
+} sawattn_kv_cache;
+
+/* Rows of heads: element e of head h of token n of sequence b at data[b*sequence + n*token + h*head + e]. */
+typedef struct sawattn_rows {
+    void* data;              /* device, 16-byte aligned */
+    int64_t sequence, token, head;      /* strides in elements: not negative, multiples of 8 */
+} sawattn_rows;
+
+#define SAWATTN_MOST_REQUESTS 4096      /* requests per call of attn_kv_pages */
+#define SAWATTN_REQUEST_ENDS (-1)       /* in new_tokens: the request's pages go back to the free list */
+
+/*
+ * attn_kv_pages -- page tables and slot maps from the lengths of the requests, built on the device.
+ * Request r holds lengths[r] rows in the pages table[r][0 .. ceil(lengths[r] / page_size)) and adds new_tokens[r] >= 0 rows.
+ * Its missing pages are taken from the front of the free list, in the order of the requests.  A request is granted its rows if
+ *   - they fit into its table row (lengths + new_tokens <= max_pages * page_size),
+ *   - the pages that it and the requests before it miss are there, and
+ *   - its tokens, counted through all requests before it, are among the first `tokens` of the batch;
+ * else it gets none of them and keeps its length.  A request with new_tokens[r] = SAWATTN_REQUEST_ENDS gives its pages
+ * back, behind the last free one (to be taken from the next call on), and its length becomes 0.
+ *
+ *   lengths, new_tokens   device, read: int32 [R], 1 <= R <= SAWATTN_MOST_REQUESTS.  Negative lengths count as 0; other negative
+ *                         values of new_tokens count as SAWATTN_REQUEST_ENDS.
+ *   table                 device, read and written: int32 [R] rows of max_pages >= 1 entries, table_stride elements apart
+ *                         (>= max_pages).  R * max_pages and max_pages * page_size must be below 2^31.  Entries of pages taken are
+ *                         written, all others left as they are (those of a request that ends, too).
+ *   page_size             a power of two, 8..2^20
+ *   free_pages            device, read and written: int32 [ring], a ring with room for every page of the cache (ring >= 1)
+ *   free_state            device, read: int32 [2] = (index of the first free page in the ring, number of free pages)
+ *   lengths_out           device, written: int32 [R], the lengths after this call
+ *   granted               device, written: int32 [R], rows granted (new_tokens[r], or 0)
+ *   token_offsets         device, written: int32 [R + 1], tokens of the batch before request r (2^31 - 1 where there are more)
+ *   free_state_out        device, written: int32 [2], free_state after this call
+ *   slots                 device, written: int64 [tokens], the slot of each token of the batch (requests in order, the tokens of
+ *                         a request in order); -1 for tokens not granted and for those behind the last request's
+ *   positions             device, written: int32 [tokens], the row (= position) of each token, -1 likewise
+ *   tokens                >= 0 (0: slots and positions may be NULL), below 2^31 - 2^20
+ * Outputs may overlap neither each other nor the inputs (a program swaps two sets of lengths and of the ring's state).
+ * One launch; no workspace.  Stream and errors as attn_fwd.
+ */
+int attn_kv_pages(const int32_t* lengths, const int32_t* new_tokens, int R, int32_t* table, int64_t table_stride, int max_pages,
+                  int page_size, int32_t* free_pages, int ring, const int32_t* free_state, int32_t* lengths_out,
+                  int32_t* granted, int32_t* token_offsets, int32_t* free_state_out, int64_t* slots, int32_t* positions,
+                  int tokens, void* hip_stream);
+
+/*
+ * attn_qkv_prepare -- what a projection's queries, keys and values go through before the attention, in one pass: each head x of
+ * Q and K becomes x / sqrt(mean(x^2) + eps) * weight, the pairs of its first `rotated` elements are turned by
+ * position * frequencies[i], and the result is written where the attention reads it.  V is copied.
+ *
+ *   q, k, v            host structs, read during the call; the rows on the device, read: [B, N] tokens of H, KH and KH heads
+ *   q_out              rows of Q, written.  May be q itself (same data and strides).
+ *   k_out, v_out       rows of K and V, written, or NULL.  May be k and v themselves.  With the strides of [B, H, N, d] these three are
+ *                      the inputs of attn_fwd.
+ *   cache, slots       both or neither NULL: row t = b*N + n of K and V is also written to slot slots[t] (device, int64 [B*N]) of
+ *                      the cache; slots outside 0 .. pages*page_size - 1 are not written.  No slot may appear twice.
+ *   positions          device, read: int32 [B*N].  A token of negative position is padding: nothing of it is read or written.
+ *   q_weight, k_weight device, read: float [d], 16-byte aligned, or NULL: the heads of Q, of K, are not normalised
+ *   eps                finite, >= 0
+ *   frequencies        device, read: double [rotated / 2], radians per position, 16-byte aligned; NULL if rotated is 0
+ *   rotated            0..d, a multiple of 8
+ *   interleaved        0: element i is paired with i + rotated/2;  non-zero: 2i with 2i + 1
+ *   B, N, H, KH        >= 1; B*N below 2^31, H + 2*KH at most 2^16
+ *   d, dtype           64 or 128, SAWATTN_F16 or SAWATTN_BF16, of all rows and of the cache
+ * Other overlaps of outputs with inputs or with each other are not allowed (and not looked for).  Angles are reduced in 64 bits, all
+ * else is computed in 32 and rounded once.  One launch; no workspace.  Stream and errors as attn_fwd.
+ */
+int attn_qkv_prepare(const sawattn_rows* q, const sawattn_rows* k, const sawattn_rows* v, const sawattn_rows* q_out,
+                     const sawattn_rows* k_out, const sawattn_rows* v_out, const sawattn_kv_cache* cache,
+                     const int64_t* slots, const int32_t* positions, const float* q_weight, const float* k_weight, float eps,
+                     const double* frequencies, int rotated, int interleaved, int B, int N, int H, int KH, int d, int dtype,
+                     void* hip_stream);
+
+/*
+ * attn_decode -- attention of one new token per request over its pages: O[r][h] = softmax(q . K^T * scale) V over the last
+ * `window` (0: all) of the lengths[r] rows that the cache holds of request r, in key/value head h / (H / cache->heads).
+ * The rows of all requests are dealt out evenly over the workgroups, long caches in pieces that a second kernel joins.
+ *
+ *   Q                  device, read: [R][H][d], element e of head h at Q[r*q_request + h*q_head + e], 16-byte aligned, type of the cache
+ *   O                  device, written, likewise with its own strides, element type o_dtype; every row of every request.  Must not
+ *                      overlap Q, the cache or the workspace.
+ *   strides            in elements, not negative, multiples of 8
+ *   cache              host struct, read during the call
+ *   table              device, read: int32 [R] rows of max_pages >= 1 entries, table_stride apart; max_pages*page_size below 2^31.
+ *                      Entries behind the length's pages are not read as pages.
+ *   lengths            device, read: int32 [R]; above max_pages*page_size they count as that, below 0 as 0
+ *   R, H               >= 1, R*H below 2^31; H a multiple of cache->heads
+ *   scale              finite
+ *   window             >= 0; only rows lengths[r] - window and later are visible; 0: all
+ *   workspace          device, written, 16-byte aligned, of at least attn_decode_workspace_bytes; used by this call's kernels only, so
+ *                      calls that overlap in time need one each.  Nothing in it has to start out zero.
+ * A request of length 0 gets zeros.  A row of the cache behind the length is never used, whatever it holds.  A table entry outside
+ * 0 .. pages - 1 among the visible ones makes the request's O NaN.  Products are exact, scores, probabilities, sums and O are held in 32 bits
+ * (the probabilities enter the second product as sums of two 16-bit numbers).  The result does not depend on timing.
+ * At most two launches.  Stream and errors as attn_fwd.
+ */
+int attn_decode(const void* Q, int64_t q_request, int64_t q_head, void* O, int64_t o_request, int64_t o_head, int o_dtype,
+                const sawattn_kv_cache* cache, const int32_t* table, int64_t table_stride, int max_pages,
+                const int32_t* lengths, int R, int H, float scale, int window, void* workspace, size_t workspace_bytes,
+                void* hip_stream);
+
+/* attn_decode_workspace_bytes -- the workspace attn_decode needs for R requests of H heads over `cache` (its pointers are not
+ * looked at) with tables of max_pages entries: a function of these numbers alone, at most some tens of MiB.  Launches nothing. */
+int attn_decode_workspace_bytes(const sawattn_kv_cache* cache, int R, int H, int max_pages, size_t* bytes);
 
 /* Text of the last error raised on the calling thread ("" if none).  Static storage, never NULL. */
 const char* attn_last_error(void);

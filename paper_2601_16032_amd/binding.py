@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -77,7 +78,7 @@ def lib() -> ctypes.CDLL:
                 f"{LIB_PATH} is not built; run `python -m paper_2601_16032_amd.build` "
                 "(or __graft_entry__.build()) first -- there is no fallback path")
         L = ctypes.CDLL(LIB_PATH)
-        vp, ci = ctypes.c_void_p, ctypes.c_int
+        vp, ci, i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
         L.attn_fwd.restype = ci
         L.attn_fwd.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ctypes.c_float, ci, ci, ci, ci, vp]
         pv = ctypes.POINTER(Variant)
@@ -96,6 +97,15 @@ def lib() -> ctypes.CDLL:
         L.attn_fwd_variant_launch_info.argtypes = [ci, ci, ci, ci, ci, ci, pv, ctypes.POINTER(LaunchInfo)]
         L.attn_fwd_plan.restype = ci
         L.attn_fwd_plan.argtypes = [ci, ci, ci, ci, ci, ci, ci, pv, vp, vp]
+        L.attn_kv_pages.restype = ci
+        L.attn_kv_pages.argtypes = [vp, vp, ci, vp, i64, ci, ci, vp, ci, vp, vp, vp, vp, vp, vp, vp, ci, vp]
+        L.attn_qkv_prepare.restype = ci
+        L.attn_qkv_prepare.argtypes = [vp] * 7 + [vp, vp, vp, vp, ctypes.c_float, vp, ci, ci, ci, ci, ci, ci, ci, ci, vp]
+        L.attn_decode.restype = ci
+        L.attn_decode.argtypes = [vp, i64, i64, vp, i64, i64, ci, vp, vp, i64, ci, vp, ci, ci, ctypes.c_float, ci, vp,
+                                  ctypes.c_size_t, vp]
+        L.attn_decode_workspace_bytes.restype = ci
+        L.attn_decode_workspace_bytes.argtypes = [vp, ci, ci, ci, ctypes.POINTER(ctypes.c_size_t)]
         for name in ("attn_last_error", "sawattn_last_error"):
             getattr(L, name).restype = ctypes.c_char_p
             getattr(L, name).argtypes = []
@@ -282,7 +292,6 @@ def attn_fwd_workspace(Q, K, V, O=None, *, scale: float, causal: bool = False, s
     return (O, tr, cnt) if trace else O
 
 
-
 def attn_fwd_static(Q, K, V, O=None, *, scale: float, causal: bool = False, scan_order="sawtooth", o_dtype=None,
                     stream=None):
     """attn_fwd with the library's fixed scratch array standing in for a workspace (the C call allocates nothing;
@@ -291,4 +300,189 @@ def attn_fwd_static(Q, K, V, O=None, *, scale: float, causal: bool = False, scan
     _check(lib().attn_fwd_static(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), B, H, N, d,
                                  float(scale), int(bool(causal)), _SCAN_CODE[scan_order],
                                  i_code, o_code, _stream(Q, stream)))
+    return O
+
+
+# ---- decoding over a paged key-value cache
+
+REQUEST_ENDS = -1        # in new_tokens of attn_kv_pages: the request's pages go back to the free list
+
+
+class _CacheStruct(ctypes.Structure):
+    """sawattn_kv_cache"""
+    _fields_ = ([("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+                + [(n, ctypes.c_int64) for n in ("k_page", "k_head", "k_row", "v_page", "v_head", "v_row")]
+                + [(n, ctypes.c_int) for n in ("pages", "page_size", "heads", "d", "dtype")])
+
+
+class KVCache:
+    """The keys and values of one layer in pages: two device tensors [pages, heads, page_size, d] of any strides whose last
+    dimension is contiguous ([pages, page_size, heads, d] as its .transpose(1, 2)).  Made once, kept with the tensors; their
+    storage must not be replaced."""
+
+    def __init__(self, k, v):
+        for name, t in (("k", k), ("v", v)):
+            if not t.is_cuda or t.dim() != 4 or t.stride(3) != 1:
+                raise ValueError(f"{name} must be a [pages, heads, page_size, d] device tensor, contiguous in its last dimension")
+        if k.shape != v.shape or k.dtype != v.dtype or k.device != v.device:
+            raise ValueError("k and v must share shape, dtype and device")
+        if k.dtype not in _IN_DTYPE_CODE:
+            raise ValueError("a cache must be float16 or bfloat16")
+        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.get_device()
+        self.pages, self.heads, self.page_size, self.d = k.shape
+        self._struct = _CacheStruct(k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3], self.pages, self.page_size,
+                                    self.heads, self.d, _IN_DTYPE_CODE[k.dtype])
+        self.ptr = ctypes.addressof(self._struct)
+
+
+def _on(device, stream, call, *args):
+    """call(*args, handle of the stream or of the device's current one) with `device` current; raises what the library refuses."""
+    if stream is not None and stream.device.index != device:
+        raise ValueError("the stream must be one of the tensors' device")
+    handle = stream.cuda_stream if stream is not None else _current_raw_stream(device)
+    if device == torch.cuda.current_device():
+        rc = call(*args, handle)
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, handle)
+    if rc != OK:
+        _check(rc)
+
+
+def _flat(name, t, dtype, n, device):
+    """Address of a contiguous tensor of n elements of this type on this device, whatever its shape."""
+    if t.dtype != dtype or not t.is_contiguous() or not t.is_cuda or t.get_device() != device or t.numel() != n:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on the other tensors' device")
+    return t.data_ptr()
+
+
+def _page_table(table, R, device):
+    """(address, stride, pages per request) of a page table"""
+    if (table.dtype != torch.int32 or not table.is_cuda or table.get_device() != device or table.dim() != 2
+            or table.shape[0] != R or table.stride(1) != 1 and table.shape[1] > 1):
+        raise ValueError("the page table must be an int32 [requests, pages] device tensor with contiguous rows")
+    wide = table.shape[1]
+    return table.data_ptr(), max(table.stride(0), wide) if R == 1 else table.stride(0), wide
+
+
+class PageStep(NamedTuple):
+    """What attn_kv_pages writes."""
+    lengths: torch.Tensor         # int32 [R]
+    granted: torch.Tensor         # int32 [R]
+    token_offsets: torch.Tensor   # int32 [R + 1]
+    free_state: torch.Tensor      # int32 [2]
+    slots: torch.Tensor           # int64 [tokens]
+    positions: torch.Tensor       # int32 [tokens]
+
+
+def attn_kv_pages(lengths, new_tokens, table, free_pages, free_state, *, page_size: int, tokens: int = None, lengths_out=None,
+                  granted=None, token_offsets=None, free_state_out=None, slots=None, positions=None, stream=None) -> PageStep:
+    """Pages, slots and positions of the tokens that `new_tokens` adds to requests of `lengths`; `table` and the ring `free_pages` are
+    brought up to date in place, the rest is written to the tensors given or to new ones (`tokens` rows where no slots are given)."""
+    R, device = lengths.numel(), lengths.get_device()
+    i32 = {"dtype": torch.int32, "device": lengths.device}
+    lengths_out = torch.empty(R, **i32) if lengths_out is None else lengths_out
+    granted = torch.empty(R, **i32) if granted is None else granted
+    token_offsets = torch.empty(R + 1, **i32) if token_offsets is None else token_offsets
+    free_state_out = torch.empty(2, **i32) if free_state_out is None else free_state_out
+    if slots is None:
+        if tokens is None:
+            raise ValueError("either slots or the number of tokens must be given")
+        slots = torch.empty(tokens, dtype=torch.int64, device=lengths.device)
+    n = slots.numel()
+    if tokens is not None and tokens != n:
+        raise ValueError("slots must hold as many elements as there are tokens")
+    positions = torch.empty(n, **i32) if positions is None else positions
+    at, stride, wide = _page_table(table, R, device)
+    _on(device, stream, (_lib or lib()).attn_kv_pages,
+        _flat("lengths", lengths, torch.int32, R, device), _flat("new_tokens", new_tokens, torch.int32, R, device), R,
+        at, stride, wide, page_size, _flat("free_pages", free_pages, torch.int32, free_pages.numel(), device),
+        free_pages.numel(), _flat("free_state", free_state, torch.int32, 2, device),
+        _flat("lengths_out", lengths_out, torch.int32, R, device), _flat("granted", granted, torch.int32, R, device),
+        _flat("token_offsets", token_offsets, torch.int32, R + 1, device),
+        _flat("free_state_out", free_state_out, torch.int32, 2, device), _flat("slots", slots, torch.int64, n, device),
+        _flat("positions", positions, torch.int32, n, device), n)
+    return PageStep(lengths_out, granted, token_offsets, free_state_out, slots, positions)
+
+
+_SixRows = ctypes.c_int64 * 24        # six of sawattn_rows: address and three strides each
+
+
+def _rows(name, t, shape, dtype, device):
+    """Address and strides of a tensor of heads, [B, N, heads, d] or [N, heads, d]."""
+    if t.shape != shape or t.dtype != dtype or not t.is_cuda or t.get_device() != device or t.stride(-1) != 1:
+        raise ValueError(f"{name} must be a {list(shape)} {dtype} tensor on the other tensors' device, contiguous in its last dimension")
+    stride = t.stride()
+    return (t.data_ptr(), stride[0], stride[1], stride[2]) if len(stride) == 4 else (t.data_ptr(), 0, stride[0], stride[1])
+
+
+def attn_qkv_prepare(q, k, v, *, positions, frequencies=None, interleaved: bool = False, q_weight=None, k_weight=None,
+                     eps: float = 1e-6, q_out=None, k_out=None, v_out=None, cache: KVCache = None, slots=None, stream=None):
+    """Norms of the heads of Q and K (where a weight is given) and rotation of their first 2 * len(frequencies) elements, K and V
+    written to `slots` of the cache and / or to k_out and v_out.  q, k, v: [B, N, heads, d] or [N, heads, d], of any strides.
+    Returns (q_out, k_out, v_out); q_out is made where it is not given, k_out and v_out where there is no cache either."""
+    if q.dim() not in (3, 4) or q.dtype not in _IN_DTYPE_CODE or not q.is_cuda:
+        raise ValueError("q must be a [B, N, H, d] or [N, H, d] device tensor, float16 or bfloat16")
+    device, dtype, shape, kv_shape = q.get_device(), q.dtype, q.shape, k.shape
+    H, KH, d, N = shape[-2], kv_shape[-2], shape[-1], shape[-3]
+    B = shape[0] if len(shape) == 4 else 1
+    if len(kv_shape) != len(shape) or kv_shape[:-2] != shape[:-2] or kv_shape[-1] != d:
+        raise ValueError("q and k must share all dimensions but the heads")
+    if (cache is None) != (slots is None) or (k_out is None) != (v_out is None):
+        raise ValueError("cache and slots, and k_out and v_out, must be given together")
+    if q_out is None:
+        q_out = torch.empty(shape, dtype=dtype, device=q.device)
+    if cache is None and k_out is None:
+        k_out, v_out = torch.empty(kv_shape, dtype=dtype, device=q.device), torch.empty(kv_shape, dtype=dtype, device=q.device)
+    if cache is not None and cache.device != device:
+        raise ValueError("the cache must be on the other tensors' device")
+    rows = _SixRows(*_rows("q", q, shape, dtype, device), *_rows("k", k, kv_shape, dtype, device),
+                    *_rows("v", v, kv_shape, dtype, device), *_rows("q_out", q_out, shape, dtype, device),
+                    *(_rows("k_out", k_out, kv_shape, dtype, device) + _rows("v_out", v_out, kv_shape, dtype, device)
+                      if k_out is not None else ()))
+    at = ctypes.addressof(rows)
+    _on(device, stream, (_lib or lib()).attn_qkv_prepare, at, at + 32, at + 64, at + 96,
+        at + 128 if k_out is not None else None, at + 160 if k_out is not None else None,
+        cache.ptr if cache is not None else None,
+        _flat("slots", slots, torch.int64, B * N, device) if slots is not None else None,
+        _flat("positions", positions, torch.int32, B * N, device),
+        _flat("q_weight", q_weight, torch.float32, d, device) if q_weight is not None else None,
+        _flat("k_weight", k_weight, torch.float32, d, device) if k_weight is not None else None, eps,
+        _flat("frequencies", frequencies, torch.float64, frequencies.numel(), device) if frequencies is not None else None,
+        2 * frequencies.numel() if frequencies is not None else 0, 1 if interleaved else 0, B, N, H, KH, d,
+        _IN_DTYPE_CODE[dtype])
+    return q_out, k_out, v_out
+
+
+def attn_decode_workspace_bytes(R: int, H: int, cache: KVCache, max_pages: int) -> int:
+    """Bytes of workspace attn_decode needs for R requests of H heads and page tables of max_pages entries."""
+    n = ctypes.c_size_t(0)
+    _check(lib().attn_decode_workspace_bytes(cache.ptr, R, H, max_pages, ctypes.byref(n)))
+    return int(n.value)
+
+
+def attn_decode(Q, cache: KVCache, table, lengths, O=None, *, scale: float, window: int = 0, o_dtype=None, workspace=None,
+                stream=None):
+    """O[r, h] = softmax(q . K^T * scale) V of one token per request, Q [R, H, d], over the last `window` (0: all) of the lengths[r]
+    cached rows that table[r] names the pages of.  workspace: a uint8 tensor of at least attn_decode_workspace_bytes bytes, made
+    here when None.  Returns O without waiting."""
+    shape, device = Q.shape, Q.get_device() if Q.is_cuda else -1
+    if len(shape) != 3 or device != cache.device or Q.dtype != cache.dtype or Q.stride(2) != 1 or shape[2] != cache.d:
+        raise ValueError("Q must be a [R, H, d] tensor of the cache's device, dtype and d, contiguous in its last dimension")
+    R, H, _ = shape
+    if O is None:
+        O = torch.empty(shape, dtype=o_dtype or Q.dtype, device=Q.device)
+    elif O.shape != shape or O.dtype not in _DTYPE_CODE or not O.is_cuda or O.get_device() != device or O.stride(2) != 1:
+        raise ValueError("O must be shaped like Q, on its device, contiguous in its last dimension (f16, bf16 or f32)")
+    if O.dtype not in _DTYPE_CODE:
+        raise ValueError("O must be float16, bfloat16 or float32")
+    at, stride, wide = _page_table(table, R, device)
+    if workspace is None:
+        workspace = torch.empty(attn_decode_workspace_bytes(R, H, cache, wide), dtype=torch.uint8, device=Q.device)
+    elif not workspace.is_cuda or workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the other tensors' device")
+    _on(device, stream, (_lib or lib()).attn_decode, Q.data_ptr(), Q.stride(0), Q.stride(1), O.data_ptr(), O.stride(0),
+        O.stride(1), _DTYPE_CODE[O.dtype], cache.ptr, at, stride, wide,
+        _flat("lengths", lengths, torch.int32, R, device), R, H, scale, window, workspace.data_ptr(),
+        workspace.numel() * workspace.element_size())
     return O

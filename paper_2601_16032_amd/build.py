@@ -54,7 +54,7 @@ def check_wide_kernels(resources: dict) -> None:
 def check_scratch(resources: dict) -> None:
     """No attention kernel uses scratch memory: what spills is stored and loaded per query tile at best, a tenth of a short launch's time.
     Refuse a build in which one does, or in which there is nothing to look at."""
-    kernels = {k: v for k, v in resources.items() if "attn_fwd_" in k}
+    kernels = {k: v for k, v in resources.items() if "attn_fwd_" in k or re.search(r"\d(?:kv_pages|qkv_prepare|decode|decode_join)_kernel", k)}
     bad = {k: v.get("ScratchSize", -1) for k, v in kernels.items() if v.get("ScratchSize", -1) != 0}
     if bad or not kernels:
         raise RuntimeError(f"attention kernels must not use scratch memory (bytes per lane): {bad or 'no kernels found'}")
@@ -62,13 +62,13 @@ def check_scratch(resources: dict) -> None:
 
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    for source, target in (("attn_fwd.hip", LIB_PATH), ("mfma_probe.hip", PROBE_LIB_PATH)):
+    for source, target in (("sawattn.hip", LIB_PATH), ("mfma_probe.hip", PROBE_LIB_PATH)):
         cmd = [hipcc, *HIPCC_FLAGS, "-Rpass-analysis=kernel-resource-usage", "-I", INCLUDE, "-I", CSRC,
                os.path.join(CSRC, source), "-o", target]
         res = subprocess.run(cmd, capture_output=True, text=True)
         if res.returncode != 0:
             raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
-        if source == "attn_fwd.hip":
+        if source == "sawattn.hip":
             try:
                 resources = kernel_resources(res.stderr)
                 check_wide_kernels(resources)

@@ -1,0 +1,264 @@
+// attn_qkv_prepare: norms of queries and keys per head, position rotation, rows to where the attention reads them.
+//
+//   y = x * rsqrt(mean(x^2) + eps) * w,   (a, b) -> (a cos t - b sin t, a sin t + b cos t),   t = position * frequency[i]
+//
+// Bound by memory: a row of d elements is read once and written once (keys and values twice where both a tensor and the cache take
+// them), at some 12 flops per element.  A row is held by d/8 lanes, eight elements each; a wavefront takes 4 (d = 128) or 8 rows
+// of one token at a time, so that the angles, the same for all heads, are made once per lane and token: four of them, the eight elements
+// being four pairs.  With pairs (i, i + rotated/2) a lane holds elements 4j.. and rotated/2 + 4j.., two pieces of 8 bytes, and no
+// element changes lanes; with pairs (2i, 2i + 1) one piece of 16 bytes.  Angles: position * frequency / 2 pi in 64 bits, less its nearest
+// whole number, which at 32 bits would be off by 0.06 of a radian at position 10^6.  Sums, norms and turns are in 32 bits, and there is one
+// rounding, to the type of the rows.
+namespace sawattn {
+
+constexpr int kPrepareThreads = 256;
+constexpr int kPrepareBatch = 4;      // rows of a lane in flight
+
+struct Rows {
+    char* data;
+    long long sequence, token, head;      // strides in bytes
+};
+
+struct PrepareParams {
+    Rows q, k, v, q_out, k_out, v_out;      // outputs with data NULL are not wanted
+    char* cache_k;                          // NULL: no cache
+    char* cache_v;
+    long long k_page, k_head, k_row, v_page, v_head, v_row;      // bytes
+    long long slots_end;
+    int shift;
+    const long long* slots;
+    const int* positions;
+    const float* q_weight;
+    const float* k_weight;
+    const double* frequencies;
+    float eps;
+    int rotated, tokens, N, H, KH, batches, chunks;      // of a token's rows a wavefront takes `batches` batches; `chunks` wavefronts take all
+};
+
+// x added up over the aligned group of LANES (8 or 16) lanes, in every lane.
+template <int LANES>
+__device__ __forceinline__ float group_sum(float x) {
+    auto moved = [](float y, auto control) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, y), decltype(control)::value, 0xf, 0xf, true));
+    };
+    x += moved(x, std::integral_constant<int, 0xb1>{});       // neighbours, quad_perm [1,0,3,2]
+    x += moved(x, std::integral_constant<int, 0x4e>{});       // pairs, quad_perm [2,3,0,1]
+    x += moved(x, std::integral_constant<int, 0x141>{});      // quads: every lane of one holds the same, so that a mirrored half row does
+    if constexpr (LANES == 16) x += moved(x, std::integral_constant<int, 0x140>{});
+    return x;
+}
+
+template <bool BF16>
+__device__ __forceinline__ float widen(unsigned word, int half) {
+    if constexpr (BF16) return __builtin_bit_cast(float, half ? word & 0xffff0000u : word << 16);
+    else return (float)__builtin_bit_cast(h2, word)[half];
+}
+
+template <bool BF16>
+__device__ __forceinline__ unsigned narrow(float a, float b) {
+    if constexpr (BF16) {
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+        return __builtin_bit_cast(unsigned, b2{(__bf16)a, (__bf16)b});
+    } else {
+        return __builtin_bit_cast(unsigned, h2{(_Float16)a, (_Float16)b});
+    }
+}
+
+template <int D, bool BF16, bool INTERLEAVED>
+__global__ __launch_bounds__(kPrepareThreads) void qkv_prepare_kernel(PrepareParams p) {
+    constexpr int kLanes = D / 8, kRows = 64 / kLanes;
+    const int lane = threadIdx.x & 63, j = lane % kLanes, group = lane / kLanes;
+    const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kPrepareThreads / 64) + (threadIdx.x >> 6));
+    const int t = unit / p.chunks, chunk = unit - t * p.chunks;
+    if (t >= p.tokens) return;
+    const int position = p.positions[t];
+    if (position < 0) return;
+    const int b = t / p.N, n = t - b * p.N;
+
+    const bool turns = j < p.rotated / 8;
+    // the lane's eight elements, in bytes: two pieces of four, or (one behind the other) one of eight
+    const int low = (INTERLEAVED || !turns) ? 16 * j : 8 * j;
+    const int high = (INTERLEAVED || !turns) ? 16 * j + 8 : p.rotated + 8 * j;
+    float cosine[4] = {1.f, 1.f, 1.f, 1.f}, sine[4] = {0.f, 0.f, 0.f, 0.f};
+    if (turns) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            double turn = (double)position * p.frequencies[4 * j + i] * 0.15915494309189533577;      // 1 / (2 pi)
+            turn -= __builtin_rint(turn);
+            sincospif(2.f * (float)turn, &sine[i], &cosine[i]);
+        }
+    }
+    f4 wq[2], wk[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int at = (i ? high : low) / 2;
+        wq[i] = p.q_weight ? *reinterpret_cast<const f4*>(p.q_weight + at) : f4{1.f, 1.f, 1.f, 1.f};
+        wk[i] = p.k_weight ? *reinterpret_cast<const f4*>(p.k_weight + at) : f4{1.f, 1.f, 1.f, 1.f};
+    }
+    long long page = -1;
+    int page_row = 0;
+    if (p.cache_k) {
+        const long long slot = p.slots[t];
+        if (slot >= 0 && slot < p.slots_end) {
+            page = slot >> p.shift;
+            page_row = (int)(slot & ((1 << p.shift) - 1));
+        }
+    }
+    auto start = [&](const Rows& rows) { return rows.data + b * rows.sequence + n * rows.token; };
+    const char* const q = start(p.q);
+    const char* const k = start(p.k);
+    const char* const v = start(p.v);
+    char* const q_out = start(p.q_out);
+    char* const k_out = p.k_out.data ? start(p.k_out) : nullptr;
+    char* const v_out = p.v_out.data ? start(p.v_out) : nullptr;
+    char* const k_slot = page >= 0 ? p.cache_k + page * p.k_page + page_row * p.k_row : nullptr;
+    char* const v_slot = page >= 0 ? p.cache_v + page * p.v_page + page_row * p.v_row : nullptr;
+
+    const int rows = p.H + 2 * p.KH;
+    for (int batch = 0; batch < p.batches; ++batch) {
+        const int row0 = (chunk * p.batches + batch) * (kRows * kPrepareBatch) + group;
+        if (row0 - group >= rows) break;
+        u2 x[kPrepareBatch][2];
+#pragma unroll
+        for (int i = 0; i < kPrepareBatch; ++i) {
+            const int row = row0 + i * kRows;
+            if (row >= rows) continue;
+            const char* from = row < p.H ? q + row * p.q.head : row < p.H + p.KH ? k + (row - p.H) * p.k.head : v + (row - p.H - p.KH) * p.v.head;
+            if constexpr (INTERLEAVED) {
+                const u4 both = *reinterpret_cast<const u4*>(from + low);
+                x[i][0] = u2{both[0], both[1]};
+                x[i][1] = u2{both[2], both[3]};
+            } else {
+                x[i][0] = *reinterpret_cast<const u2*>(from + low);
+                x[i][1] = *reinterpret_cast<const u2*>(from + high);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kPrepareBatch; ++i) {
+            const int row = row0 + i * kRows;
+            if (row >= rows) continue;
+            const bool is_q = row < p.H, is_v = row >= p.H + p.KH;
+            if (!is_v) {
+                float y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = widen<BF16>(x[i][e / 4][e / 2 % 2], e % 2);
+                if (is_q ? p.q_weight != nullptr : p.k_weight != nullptr) {
+                    float square = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) square += y[e] * y[e];
+                    const float norm = 1.f / sqrtf(group_sum<kLanes>(square) * (1.f / D) + p.eps);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] *= norm * (is_q ? wq[e / 4][e % 4] : wk[e / 4][e % 4]);
+                }
+                if (turns) {
+#pragma unroll
+                    for (int i2 = 0; i2 < 4; ++i2) {
+                        const int ea = INTERLEAVED ? 2 * i2 : i2, eb = INTERLEAVED ? 2 * i2 + 1 : i2 + 4;
+                        const float a = y[ea], c = y[eb];
+                        y[ea] = a * cosine[i2] - c * sine[i2];
+                        y[eb] = a * sine[i2] + c * cosine[i2];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) x[i][e / 4][e / 2 % 2] = narrow<BF16>(y[e], y[e + 1]);
+            }
+            auto put = [&](char* to) {
+                if constexpr (INTERLEAVED) {
+                    *reinterpret_cast<u4*>(to + low) = u4{x[i][0][0], x[i][0][1], x[i][1][0], x[i][1][1]};
+                } else {
+                    *reinterpret_cast<u2*>(to + low) = x[i][0];
+                    *reinterpret_cast<u2*>(to + high) = x[i][1];
+                }
+            };
+            if (is_q) {
+                put(q_out + row * p.q_out.head);
+            } else if (!is_v) {
+                const int head = row - p.H;
+                if (k_out) put(k_out + head * p.k_out.head);
+                if (k_slot) put(k_slot + head * p.k_head);
+            } else {
+                const int head = row - p.H - p.KH;
+                if (v_out) put(v_out + head * p.v_out.head);
+                if (v_slot) put(v_slot + head * p.v_head);
+            }
+        }
+    }
+}
+
+template <int D, bool BF16>
+void launch_prepare(const PrepareParams& p, bool interleaved, int grid, hipStream_t stream) {
+    if (interleaved) hipLaunchKernelGGL((qkv_prepare_kernel<D, BF16, true>), dim3(grid), dim3(kPrepareThreads), 0, stream, p);
+    else hipLaunchKernelGGL((qkv_prepare_kernel<D, BF16, false>), dim3(grid), dim3(kPrepareThreads), 0, stream, p);
+}
+
+}  // namespace sawattn
+
+extern "C" int attn_qkv_prepare(const sawattn_rows* q, const sawattn_rows* k, const sawattn_rows* v, const sawattn_rows* q_out,
+                                const sawattn_rows* k_out, const sawattn_rows* v_out, const sawattn_kv_cache* cache,
+                                const int64_t* slots, const int32_t* positions, const float* q_weight, const float* k_weight,
+                                float eps, const double* frequencies, int rotated, int interleaved, int B, int N, int H, int KH,
+                                int d, int dtype, void* hip_stream) {
+    using namespace sawattn;
+    if (B <= 0 || N <= 0 || H <= 0 || KH <= 0 || d <= 0) return fail(SAWATTN_ERR_INVALID_ARG, "B, N, H, KH and d must be positive");
+    if (d != 64 && d != 128) return fail(SAWATTN_ERR_UNSUPPORTED, "head dimension must be 64 or 128");
+    if (dtype != SAWATTN_F16 && dtype != SAWATTN_BF16)
+        return fail(SAWATTN_ERR_INVALID_ARG, "dtype must be SAWATTN_F16 or SAWATTN_BF16");
+    if ((long long)B * N >= (1LL << 31) || H > (1 << 16) || KH > (1 << 16) || H + 2LL * KH > (1 << 16))
+        return fail(SAWATTN_ERR_INVALID_ARG, "B*N must be below 2^31 and H + 2*KH at most 2^16");
+    if (rotated < 0 || rotated > d || rotated % 8) return fail(SAWATTN_ERR_INVALID_ARG, "rotated must be a multiple of 8 from 0 to d");
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(SAWATTN_ERR_INVALID_ARG, "eps must be finite and not negative");
+    if (!q || !k || !v || !q_out || !positions || (rotated && !frequencies))
+        return fail(SAWATTN_ERR_INVALID_ARG, "q, k, v, q_out, positions and (with rotated > 0) frequencies must be non-null");
+    if ((k_out == nullptr) != (v_out == nullptr)) return fail(SAWATTN_ERR_INVALID_ARG, "k_out and v_out must be given together");
+    if ((cache == nullptr) != (slots == nullptr)) return fail(SAWATTN_ERR_INVALID_ARG, "cache and slots must be given together");
+    if (((uintptr_t)q_weight | (uintptr_t)k_weight | (uintptr_t)frequencies) & 15u)
+        return fail(SAWATTN_ERR_INVALID_ARG, "q_weight, k_weight and frequencies must be 16-byte aligned");
+    if (((uintptr_t)positions & 3u) || ((uintptr_t)slots & 7u))
+        return fail(SAWATTN_ERR_INVALID_ARG, "positions and slots must be aligned to their elements");
+    PrepareParams p{};
+    const struct { const sawattn_rows* from; Rows* to; int heads; } tensors[] = {
+        {q, &p.q, H}, {k, &p.k, KH}, {v, &p.v, KH}, {q_out, &p.q_out, H}, {k_out, &p.k_out, KH}, {v_out, &p.v_out, KH}};
+    for (int i = 0; i < 6; ++i) {
+        const sawattn_rows* s = tensors[i].from;
+        if (!s) continue;
+        if (!s->data || ((uintptr_t)s->data & 15u)) return fail(SAWATTN_ERR_INVALID_ARG, "rows must be non-null and 16-byte aligned");
+        if (!good_stride(s->sequence, B) || !good_stride(s->token, N) || !good_stride(s->head, tensors[i].heads))
+            return fail(SAWATTN_ERR_INVALID_ARG, "strides of rows must be multiples of 8, not negative");
+        // rows written must be rows of their own
+        if (i >= 3 && ((B > 1 && s->sequence < d) || (N > 1 && s->token < d) || (tensors[i].heads > 1 && s->head < d)))
+            return fail(SAWATTN_ERR_INVALID_ARG, "strides of rows that are written must be at least d");
+        *tensors[i].to = {static_cast<char*>(s->data), 2 * s->sequence, 2 * s->token, 2 * s->head};
+    }
+    if (cache) {
+        const int rc = check_cache(cache, true);
+        if (rc != SAWATTN_OK) return rc;
+        if (cache->heads != KH || cache->d != d || cache->dtype != dtype)
+            return fail(SAWATTN_ERR_INVALID_ARG, "the cache's heads, d and dtype must be those of K and V");
+        for (const int64_t* s : {&cache->k_page, &cache->v_page})      // page, head and row strides lie one behind the other
+            if ((cache->pages > 1 && s[0] < d) || (KH > 1 && s[1] < d) || s[2] < d)
+                return fail(SAWATTN_ERR_INVALID_ARG, "strides of a cache that is written must be at least d");
+        p.cache_k = static_cast<char*>(cache->k);
+        p.cache_v = static_cast<char*>(cache->v);
+        p.k_page = 2 * cache->k_page; p.k_head = 2 * cache->k_head; p.k_row = 2 * cache->k_row;
+        p.v_page = 2 * cache->v_page; p.v_head = 2 * cache->v_head; p.v_row = 2 * cache->v_row;
+        p.shift = page_shift(cache->page_size);
+        p.slots_end = (long long)cache->pages << p.shift;
+        p.slots = reinterpret_cast<const long long*>(slots);
+    }
+    p.positions = positions;
+    p.q_weight = q_weight; p.k_weight = k_weight; p.frequencies = frequencies;
+    p.eps = eps; p.rotated = rotated; p.tokens = B * N; p.N = N; p.H = H; p.KH = KH;
+    // A wavefront takes all rows of a token, or, where that would leave compute units without work, fewer: down to one batch.
+    const int rows = H + 2 * KH, per_batch = kPrepareBatch * 64 / (d / 8), all = (rows + per_batch - 1) / per_batch;
+    const int wanted = (int)std::min<long long>(all, (2048 + p.tokens - 1) / p.tokens);
+    p.batches = (all + wanted - 1) / wanted;
+    p.chunks = (all + p.batches - 1) / p.batches;
+    const long long waves = (long long)p.tokens * p.chunks;
+    if (waves >= (1LL << 31) - kPrepareThreads / 64) return fail(SAWATTN_ERR_INVALID_ARG, "too many tokens");
+    const int grid = (int)((waves + kPrepareThreads / 64 - 1) / (kPrepareThreads / 64));
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const bool bf = dtype == SAWATTN_BF16;
+    if (d == 128) bf ? launch_prepare<128, true>(p, interleaved != 0, grid, stream) : launch_prepare<128, false>(p, interleaved != 0, grid, stream);
+    else bf ? launch_prepare<64, true>(p, interleaved != 0, grid, stream) : launch_prepare<64, false>(p, interleaved != 0, grid, stream);
+    return launched("attn_qkv_prepare");
+}
