@@ -311,7 +311,7 @@ typedef struct sawattn_kv_cache {
     int64_t k_page, k_head, k_row;      /* strides in elements: not negative, multiples of 8 */
     int64_t v_page, v_head, v_row;
     int pages;               /* >= 1 */
-    int page_size;           /* rows per page: a power of two, 8..2^20 */
+    int page_size;           /* rows per page: a power of two, 16..2^20 */
     int heads;               /* key/value heads, >= 1 */
     int d;                   /* head dimension, 64 or 128; its elements lie side by side */
     int dtype;               /* SAWATTN_F16 or SAWATTN_BF16 */
@@ -341,7 +341,7 @@ typedef struct sawattn_rows {
  *   table                 device, read and written: int32 [R] rows of max_pages >= 1 entries, table_stride elements apart
  *                         (>= max_pages).  R * max_pages and max_pages * page_size must be below 2^31.  Entries of pages taken are
  *                         written, all others left as they are (those of a request that ends, too).
- *   page_size             a power of two, 8..2^20
+ *   page_size             a power of two, 16..2^20
  *   free_pages            device, read and written: int32 [ring], a ring with room for every page of the cache (ring >= 1)
  *   free_state            device, read: int32 [2] = (index of the first free page in the ring, number of free pages)
  *   lengths_out           device, written: int32 [R], the lengths after this call
@@ -397,19 +397,21 @@ int attn_qkv_prepare(const sawattn_rows* q, const sawattn_rows* k, const sawattn
  *   O                  device, written, likewise with its own strides, element type o_dtype; every row of every request.  Must not
  *                      overlap Q, the cache or the workspace.
  *   strides            in elements, not negative, multiples of 8
- *   cache              host struct, read during the call
- *   table              device, read: int32 [R] rows of max_pages >= 1 entries, table_stride apart; max_pages*page_size below 2^31.
+ *   cache              host struct, read during the call; row strides at most 2^26
+ *   table              device, read: int32 [R] rows of max_pages >= 1 entries, table_stride apart; max_pages*page_size at most 2^30,
+ *                      R*H*ceil(max_pages*page_size/128) below 2^31 - 2048.
  *                      Entries behind the length's pages are not read as pages.
  *   lengths            device, read: int32 [R]; above max_pages*page_size they count as that, below 0 as 0
  *   R, H               >= 1, R*H below 2^31; H a multiple of cache->heads
  *   scale              finite
  *   window             >= 0; only rows lengths[r] - window and later are visible; 0: all
- *   workspace          device, written, 16-byte aligned, of at least attn_decode_workspace_bytes; used by this call's kernels only, so
+ *   workspace          device, written, 16-byte aligned, of at least attn_decode_workspace_bytes (NULL where that is 0); used by this call's kernels only, so
  *                      calls that overlap in time need one each.  Nothing in it has to start out zero.
  * A request of length 0 gets zeros.  A row of the cache behind the length is never used, whatever it holds.  A table entry outside
  * 0 .. pages - 1 among the visible ones makes the request's O NaN.  Products are exact, scores, probabilities, sums and O are held in 32 bits
  * (the probabilities enter the second product as sums of two 16-bit numbers).  The result does not depend on timing.
- * At most two launches.  Stream and errors as attn_fwd.
+ * One launch where the rows that can be visible are few (up to 256 KiB of K and V per request and key/value head, or 1 MiB with
+ * 256 of those and more), else two.  Stream and errors as attn_fwd.
  */
 int attn_decode(const void* Q, int64_t q_request, int64_t q_head, void* O, int64_t o_request, int64_t o_head, int o_dtype,
                 const sawattn_kv_cache* cache, const int32_t* table, int64_t table_stride, int max_pages,

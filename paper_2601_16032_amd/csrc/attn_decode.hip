@@ -3,29 +3,40 @@
 //   s_j = scale q . k_j,  o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m)   over the visible rows j of a request
 //
 // Bound by memory: every key and value is read once, for 4 d flops per query head that shares it.  A unit is a request, a key/value
-// head and up to 16 of its query heads; its rows are cut into tiles of 32.  The tiles of all units, one behind the other, are dealt
-// out evenly: workgroup w of G takes `share` of them from w * share on, whatever the lengths are, so that one long request and many
-// short ones load the chip alike and the launch needs to know no length on the host.  Where a unit is spread over workgroups each leaves
-// (m, sum, O) of its part in the workspace, and a second kernel joins them.  A workgroup ends at most two units unfinished, its first and
-// its last, so the workspace has two places per workgroup.
+// head and up to 16 of its query heads.
 //
-// Within a workgroup the four wavefronts take every fourth tile, each with its own running maximum and sum, and are added up in LDS at the
+// Who does what.  Where a unit is short (below) a workgroup of eight wavefronts takes all of it: one launch.  Else the units' rows are cut into steps
+// of 128, and the steps of all units, one behind the other, are dealt out evenly: workgroup w takes `share` of them from w * share on, whatever the
+// lengths are, so that one long request and many short ones load the chip alike and the host needs to know no length.  A workgroup ends at
+// most two units unfinished, its first and its last; of those it leaves (m, sum, O) of its part in one of its two places in the workspace,
+// and a second kernel joins them.  Measured (16 x 32768, ungrouped): 256, 512, 1024 and 2048 workgroups 660, 660, 670 and 690 us; ragged requests want
+// two workgroups to a compute unit, so that one loads while the other ends a unit (64 requests up to 8192: 95 us, one of eight wavefronts 103).
+//
+// Within a workgroup every wavefront takes tiles of 32 keys of its own, with its own running maximum and sum; they are added up in LDS at the
 // unit's end.  Products run on 16x16x32 MFMAs, transposed: S^T = K Q^T, O^T = V^T P^T with the 16 columns the query heads (columns without
-// one are computed and dropped: the matrix cores idle anyway).  K goes from memory straight into A operands.  In the result a lane holds
-// eight scores of one head: four rows of S^T in each of two MFMAs.  With row i + 4 g + 16 mt of the two standing for key 8 g + 4 mt + i,
-// these are keys 8 g .. 8 g + 7, which is what the lane has to hold of P^T as B operand of the second product: probabilities stay where
-// they are.  V comes as eight rows of a lane group's keys, 16 bytes (8 bytes at d = 64) of each per lane; pairs of rows are interleaved in
-// registers (v_perm) into A operands whose MFMA j has the elements j, j + 8, ... of V: neither K nor V passes LDS.
+// one are computed and dropped: the matrix cores idle anyway).  K passes through LDS, by direct loads of whole rows: read from memory in
+// the operands' order, 64 bytes of 16 rows at a time, it took 5 % longer.  In the result a lane (c = lane % 16, g = lane / 16) holds eight scores of
+// head c: rows 4 g + i of two MFMAs.  Row 4 g + i stands for key 4 i + g of 16, so that the lane's eight keys are those of which it
+// has to hold the probabilities as B operand of the second product: they stay where they are.  V comes as rows 4 i + g, 16 bytes (8 at d = 64)
+// of each per lane, four whole rows per load, and never leaves the registers: pairs of rows are interleaved (v_perm) into A operands, whose MFMA j
+// has elements j, j + D/16, ... of V.
 //
 // The probabilities enter the second product as the sum of two 16-bit numbers, so that they are not rounded: the matrix cores have time
 // for both.  Binary16 ones are scaled by 2^12 for the sake of small ones.
+//
+// K and V are read with non-temporal loads (7.1 instead of 6.3 TB/s for a kernel that only reads).  Measured with the products taken out,
+// the loads of 16 x 32768 take 655 us (pages of 16 rows in any order; of 256 rows: 645), with them 660: 6.5 TB/s.  Loading a tile ahead, in
+// registers, gave nothing: four wavefronts on each of four SIMDs keep enough on its way.
 namespace sawattn {
 
-constexpr int kDecodeThreads = 256, kDecodeWaves = kDecodeThreads / 64;
-constexpr int kDecodeTile = 32;           // keys of a tile
-constexpr int kDecodeHeads = 16;          // query heads of a unit
-constexpr int kDecodeGrid = 1024;         // workgroups at most
-constexpr int kDecodeLeast = 8;           // tiles of a workgroup at least
+constexpr int kDecodeWaves = 4;                                  // of a workgroup that shares units with others
+constexpr int kDecodeTile = 32;                                  // keys a wavefront takes at a time
+constexpr int kDecodeStep = kDecodeTile * kDecodeWaves;          // keys such a workgroup takes at a time: what is dealt out
+constexpr int kDecodeHeads = 16;                                 // query heads of a unit
+constexpr int kDecodeDirectWaves = 8;                            // of a workgroup that takes whole units
+constexpr long long kDecodeDirectFew = 1 << 18, kDecodeDirectMany = 1 << 20;      // bytes of K and V of a unit at most, with fewer or more units than compute units
+constexpr int kDecodeGrid = 1024;                                // workgroups that share units: at most
+constexpr int kDecodeUnits = 256;                                // compute units: up to as many workgroups of one step, then of two at least
 
 struct DecodeParams {
     const char* Q;
@@ -33,12 +44,14 @@ struct DecodeParams {
     long long q_request, q_head, o_request, o_head;      // bytes
     const char* K;
     const char* V;
-    long long k_page, k_head, k_row, v_page, v_head, v_row;      // bytes
+    long long k_page, k_head, v_page, v_head;            // bytes
+    unsigned k_row, v_row;
     const int* table;
     long long table_stride;
     const int* lengths;
     float* parts;        // workspace: [2 * grid][heads_kept][D] of O
     f2* part_sums;       // [2 * grid][heads_kept] of (maximum, sum)
+    int4* begun;         // [grid] the unit that the workgroup leaves for others to end: (request, unit, workgroup that ends it, 0); request -1: none
     float c;             // scale * log2(e)
     int o_dtype, R, capacity, window, pages, shift;
     int group;           // query heads per key/value head
@@ -48,43 +61,61 @@ struct DecodeParams {
 };
 
 struct DecodeRequest {
-    int length, low, first, tiles;      // visible rows low .. length - 1, in tiles from `first` on
+    int length, low, first, steps;      // visible rows low .. length - 1, in steps from `first` on
     __device__ __forceinline__ DecodeRequest(const DecodeParams& p, int given) {
         length = min(max(given, 0), p.capacity);
         low = p.window ? max(length - p.window, 0) : 0;
-        first = low / kDecodeTile;
-        tiles = length ? (length - 1) / kDecodeTile - first + 1 : 0;
+        first = low / kDecodeStep;
+        steps = length ? (length - 1) / kDecodeStep - first + 1 : 0;
     }
 };
 
-__device__ __forceinline__ long long divide(long long a, long long b) {      // of numbers that are not negative, mostly of few bits
-    if (((a | b) >> 31) == 0) return (unsigned)a / (unsigned)b;
-    return a / b;
+// Sum over the lanes up to and including this one.
+__device__ __forceinline__ int lanes_upto(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8: within rows of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // the last lane of rows 0 and 2 into rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // lane 31 into rows 2 and 3
+    return x;
 }
 
-// How the tiles are dealt out: the same in both kernels, from the lengths alone.  Every wavefront works it out for itself.
-struct DecodeShares {
-    long long share;
-    // ALL: the sum over all requests gives the share; tiles of the requests before request `of` (if not negative) in `before`
-    long long before;
-    __device__ __forceinline__ DecodeShares(const DecodeParams& p, int lane, int grid, int of) {
-        long long all = 0, ahead = 0;
-        for (int r = lane; r < p.R; r += 64) {
-            const int n = DecodeRequest(p, p.lengths[r]).tiles;
-            all += n;
-            if (r < of) ahead += n;
+// How the steps are dealt out, from the lengths alone: what workgroup `wg` of `grid` has to do.  Every wavefront works it out for itself.
+struct DecodeShare {
+    int share;                 // steps of a workgroup
+    int left;                  // of this one: none if not positive
+    int r, unit, t0;           // the first one: request, unit of the request, step of the unit
+    int length;                // lengths[r]
+    __device__ __forceinline__ DecodeShare(const DecodeParams& p, int lane, int wg, int grid) {
+        // the first 64 lengths stay in registers: mostly there are no more, and a second trip to memory would cost as much as a step
+        const int given0 = lane < p.R ? p.lengths[lane] : 0;
+        int all = DecodeRequest(p, given0).steps;
+        for (int i = lane + 64; i < p.R; i += 64) all += DecodeRequest(p, p.lengths[i]).steps;
+        const int total = __builtin_amdgcn_readlane(lanes_upto(all), 63) * p.units;
+        share = max((int)(((unsigned)total + grid - 1) / (unsigned)grid), total > kDecodeUnits ? 2 : 1);
+        const int at = wg * share;      // (below the total and twice the grid)
+        left = min(share, total - at);
+        r = unit = t0 = length = 0;
+        if (left <= 0) return;
+        const int wanted = (unsigned)at / (unsigned)p.units;
+        int before = 0;      // steps of the requests in front
+        for (int r0 = 0;; r0 += 64) {
+            const int given = r0 == 0 ? given0 : r0 + lane < p.R ? p.lengths[r0 + lane] : 0;
+            const int steps = DecodeRequest(p, given).steps, upto = lanes_upto(steps);
+            const unsigned long long found = __ballot(before + upto > wanted);
+            if (found) {
+                const int here = __builtin_ctzll(found), of_request = __builtin_amdgcn_readlane(steps, here);
+                r = r0 + here;
+                length = __builtin_amdgcn_readlane(given, here);
+                const int inside = at - (before + __builtin_amdgcn_readlane(upto, here) - of_request) * p.units;      // below units * steps of the request
+                unit = (unsigned)inside / (unsigned)of_request;
+                t0 = inside - unit * of_request;
+                return;
+            }
+            before += __builtin_amdgcn_readlane(upto, 63);
         }
-#pragma unroll
-        for (int step = 1; step < 64; step *= 2) {
-            all += __shfl_xor(all, step);
-            ahead += __shfl_xor(ahead, step);
-        }
-        share = divide(all * p.units + grid - 1, grid);
-        share = max((long long)kDecodeLeast, (share + kDecodeWaves - 1) / kDecodeWaves * kDecodeWaves);
-        before = ahead;
-        total = all * p.units;
     }
-    long long total;
 };
 
 template <bool BF16>
@@ -93,46 +124,63 @@ __device__ __forceinline__ f4 decode_mfma(u4 a, u4 b, f4 c) {
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
 }
 
+// The larger, and the sum, of x in the four lanes that hold a head.
+__device__ __forceinline__ void lane_quarters(float x, float& one, float& other) {      // neighbouring rows of 16 lanes exchanged
+    unsigned a = __builtin_bit_cast(unsigned, x), b = a;
+    asm volatile("s_nop 1\n\tv_permlane16_swap_b32 %0, %1\n\ts_nop 1" : "+v"(a), "+v"(b));
+    one = __builtin_bit_cast(float, a);
+    other = __builtin_bit_cast(float, b);
+}
+__device__ __forceinline__ float head_max(float x) {
+    float one, other;
+    lane_quarters(x, one, other);
+    return pair_max(fmaxf(one, other));
+}
+__device__ __forceinline__ float head_sum(float x) {
+    float one, other;
+    lane_quarters(x, one, other);
+    return pair_sum(one + other);
+}
+
+// A tile's way through LDS and registers; lane constants.  16-byte pieces of a row of K change places in LDS (by exclusive or with the
+// row's number: `turn`), so that 16 lanes reading the same piece of 16 rows find it in all banks; the lane that loads a piece fetches the
+// one that belongs there.
+template <int D>
+struct DecodeLane {
+    static constexpr int kRowBytes = 2 * D, kLoads = kDecodeTile * kRowBytes / 1024, kPieces = kRowBytes / 16, kRowsPerLoad = 64 / kPieces;
+    int c, g;
+    unsigned k_row, k_piece;      // the lane's row and piece of a load of K, in bytes
+    unsigned v_from;              // byte offset of its piece in the four rows of a load of V
+    int k_at;                     // in the tile in LDS: its A operands of the first 16 keys, first 32 elements
+    __device__ __forceinline__ DecodeLane(const DecodeParams& p, int lane) {
+        c = lane & 15;
+        g = lane >> 4;
+        k_row = lane / kPieces * p.k_row;
+        k_piece = (lane % kPieces ^ turn(lane / kPieces)) * 16;
+        v_from = g * p.v_row + c * (D / 8);
+        const int mine = 4 * (c & 3) + (c >> 2);      // of 16 keys the one whose scores are row c of the product
+        k_at = mine * kRowBytes + (g ^ turn(mine)) * 16;
+    }
+    static __device__ __forceinline__ int turn(int row) { return D == 128 ? row & 15 : row >> 1 & 7; }
+    // Load i of a tile fetches rows from i * kRowsPerLoad on, whose numbers have no bit in common with a lane's row in them.
+    __device__ __forceinline__ unsigned k_from(int i) const { return k_row + (k_piece ^ turn(i * kRowsPerLoad) * 16); }
+    // Elements 32 x .. of the operand are the lane's 16-byte pieces 4 x + g.
+    __device__ __forceinline__ int k_operand(int x) const { return k_at ^ x * 64; }
+};
+
 // What a unit's tiles need of its request and head.
 struct DecodeUnit {
     const char* K;
     const char* V;
-    const int* pages;
+    const __attribute__((address_space(4))) int* pages;      // (through the scalar cache: a tile's two pages are the wavefront's)
     int low, length;
 };
 
-template <int D>
-struct DecodeTile {
-    u4 k[2][D / 32];            // A operands: [rows of S^T][32 elements]
-    unsigned v[8][D / 32];      // eight rows of V, D / 32 words of each
-    bool bad_k, bad_v;
-
-    __device__ __forceinline__ void load(const DecodeParams& p, const DecodeUnit& u, int tile, int lane) {
-        const int c = lane & 15, g = lane >> 4;
-        const int key_k = tile * kDecodeTile + c / 4 * 8, key_v = tile * kDecodeTile + g * 8, mask = (1 << p.shift) - 1;
-        int page_k = u.pages[min(key_k, u.length - 1) >> p.shift], page_v = u.pages[min(key_v, u.length - 1) >> p.shift];
-        bad_k = (unsigned)page_k >= (unsigned)p.pages;
-        bad_v = (unsigned)page_v >= (unsigned)p.pages;
-        if (bad_k) page_k = 0;
-        if (bad_v) page_v = 0;
-        const char* at_k = u.K + page_k * p.k_page + ((key_k & mask) + c % 4) * p.k_row + g * 16;
+struct DecodePages {      // of the two halves of a tile
+    int half[2];
+    __device__ __forceinline__ DecodePages(const DecodeParams& p, const DecodeUnit& u, int tile) {
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-            for (int s = 0; s < D / 32; ++s) k[mt][s] = *reinterpret_cast<const u4*>(at_k + mt * 4 * p.k_row + s * 64);
-        const char* at_v = u.V + page_v * p.v_page + (key_v & mask) * p.v_row + c * (D / 8);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (D == 128) {
-                const u4 w = *reinterpret_cast<const u4*>(at_v + i * p.v_row);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) v[i][x] = w[x];
-            } else {
-                const u2 w = *reinterpret_cast<const u2*>(at_v + i * p.v_row);
-#pragma unroll
-                for (int x = 0; x < 2; ++x) v[i][x] = w[x];
-            }
-        }
+        for (int i = 0; i < 2; ++i) half[i] = u.pages[min(tile * kDecodeTile + i * 16, u.length - 1) >> p.shift];
     }
 };
 
@@ -148,30 +196,63 @@ struct DecodeState {
         l = 0.f;
     }
 
-    __device__ __forceinline__ void add(const DecodeParams& p, const DecodeUnit& u, const u4 (&q)[D / 32], DecodeTile<D>& t, int tile, int lane) {
-        const int g = lane >> 4, key0 = tile * kDecodeTile + g * 8;
+    __device__ __forceinline__ void add(const DecodeParams& p, const DecodeLane<D>& lane, const DecodeUnit& u, const u4 (&q)[D / 32], const DecodePages& pages, int tile,
+                                        LDS_PTR(char) lds) {
+        using L = DecodeLane<D>;
+        const int mask = (1 << p.shift) - 1, key0 = tile * kDecodeTile;
+        bool bad[2];
+        unsigned v[8][D / 32];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            bad[half] = (unsigned)pages.half[half] >= (unsigned)p.pages;
+            const int page = bad[half] ? 0 : pages.half[half], row = (key0 + half * 16) & mask;
+            const char* k = u.K + page * p.k_page + (long long)row * p.k_row;
+#pragma unroll
+            for (int i = 0; i < L::kLoads / 2; ++i)
+                load_to_lds_16B_nt(k + (long long)i * L::kRowsPerLoad * p.k_row, lane.k_from(i),
+                                   (unsigned)(uintptr_t)lds + (half * (L::kLoads / 2) + i) * 1024);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int page = bad[half] ? 0 : pages.half[half], row = (key0 + half * 16) & mask;
+            const char* from = u.V + page * p.v_page + (long long)row * p.v_row;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const char* at = from + (long long)i * 4 * p.v_row;
+                if constexpr (D == 128) {
+                    const u4 w = __builtin_nontemporal_load(reinterpret_cast<const u4*>(at + lane.v_from));
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) v[half * 4 + i][x] = w[x];
+                } else {
+                    const u2 w = __builtin_nontemporal_load(reinterpret_cast<const u2*>(at + lane.v_from));
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) v[half * 4 + i][x] = w[x];
+                }
+            }
+        }
+        wait_tile_landed();
         f4 s[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int x = 0; x < D / 32; ++x)
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt) s[mt] = decode_mfma<BF16>(t.k[mt][x], q[x], s[mt]);
+            for (int half = 0; half < 2; ++half)
+                s[half] = decode_mfma<BF16>(*(LDS_PTR(const u4))(lds + lane.k_operand(x) + half * 16 * L::kRowBytes), q[x], s[half]);
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) s[mt] *= p.c;
-        const bool edge = tile * kDecodeTile < u.low || (tile + 1) * kDecodeTile > u.length;
-        if (edge || __any(t.bad_v)) {
+        for (int half = 0; half < 2; ++half) s[half] *= p.c;
+        if (key0 < u.low || key0 + kDecodeTile > u.length || bad[0] || bad[1]) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool seen = key0 + i >= u.low && key0 + i < u.length;
-                s[i / 4][i % 4] = !seen ? -INFINITY : t.bad_v ? __builtin_nanf("") : s[i / 4][i % 4];
+                const int key = key0 + 4 * i + lane.g;
+                const bool seen = key >= u.low && key < u.length;
+                s[i / 4][i % 4] = !seen ? -INFINITY : bad[i / 4] ? __builtin_nanf("") : s[i / 4][i % 4];
                 if (!seen) {      // whatever the row holds, it takes no part: 0 * NaN would
 #pragma unroll
-                    for (int x = 0; x < D / 32; ++x) t.v[i][x] = 0;
+                    for (int x = 0; x < D / 32; ++x) v[i][x] = 0;
                 }
             }
         }
         float most = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-        most = fmaxf(most, __shfl_xor(most, 16));
-        most = fmaxf(most, __shfl_xor(most, 32));
+        most = head_max(most);
         if (__any(most > m)) {
             const float next = fmaxf(m, most), fade = next == -INFINITY ? 1.f : fast_exp2(m - next);
             m = next;
@@ -191,9 +272,9 @@ struct DecodeState {
         }
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
-            u4 a;      // element j of the lane's pieces of the eight rows
+            u4 a;      // element j of the lane's pieces of its eight rows
 #pragma unroll
-            for (int w = 0; w < 4; ++w) a[w] = __builtin_amdgcn_perm(t.v[2 * w + 1][j / 2], t.v[2 * w][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+            for (int w = 0; w < 4; ++w) a[w] = __builtin_amdgcn_perm(v[2 * w + 1][j / 2], v[2 * w][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
             o[j] = decode_mfma<BF16>(a, high, o[j]);
             o[j] = decode_mfma<BF16>(a, rest, o[j]);
         }
@@ -206,198 +287,231 @@ __device__ __forceinline__ void store_o(char* to, int dtype, f4 x) {
     else *reinterpret_cast<u2*>(to) = u2{narrow<false>(x[0], x[1]), narrow<false>(x[2], x[3])};
 }
 
-template <int D, bool BF16>
-__global__ __launch_bounds__(kDecodeThreads) void decode_kernel(DecodeParams p) {
-    constexpr int kPitch = D + 4;      // (rows of 16 lanes' pieces start in different banks)
-    __shared__ __align__(16) float o_of[kDecodeWaves][kDecodeHeads][kPitch];
-    __shared__ float m_of[kDecodeWaves][kDecodeHeads], l_of[kDecodeWaves][kDecodeHeads];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
-    const int grid = gridDim.x;
+// DIRECT: a workgroup takes a unit, all of it; else what its number says of all units.
+template <int D, bool BF16, int WAVES, bool DIRECT>
+__global__ __launch_bounds__(64 * WAVES, 4) void decode_kernel(DecodeParams p) {
+    static_assert(DIRECT || WAVES == kDecodeWaves, "shares are counted in steps of that many wavefronts");
+    constexpr int kPitch = D + 4;      // floats of a head's O in LDS (rows of 16 lanes' pieces start in different banks)
+    constexpr int kArea = kDecodeHeads * kPitch * 4;      // of a wavefront: its tile of K, and at a unit's end its O
+    static_assert(kArea >= kDecodeTile * 2 * D, "a tile of K fits");
+    __shared__ __align__(16) char area[WAVES][kArea];
+    __shared__ float m_of[WAVES][kDecodeHeads], l_of[WAVES][kDecodeHeads];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const DecodeLane<D> lane(p, tid & 63);
 
-    const DecodeShares shares(p, lane, grid, -1);
-    long long at = blockIdx.x * shares.share;
-    const long long end = min(at + shares.share, shares.total);
-    if (at >= end) return;
-
-    // the request that holds tile `at`, and how many tiles of the requests go before it
-    int r = 0;
-    long long before = 0;
-    const long long wanted = divide(at, p.units);
-    for (int r0 = 0; r0 < p.R; r0 += 64) {
-        const int n = r0 + lane < p.R ? DecodeRequest(p, p.lengths[r0 + lane]).tiles : 0;
-        long long upto = n;
-#pragma unroll
-        for (int step = 1; step < 64; step *= 2) {
-            const long long x = __shfl_up(upto, step);
-            if (lane >= step) upto += x;
+    int r, unit, t0, left, share, length;
+    if constexpr (DIRECT) {
+        r = blockIdx.x / p.units;
+        unit = blockIdx.x - r * p.units;
+        t0 = left = share = 0;
+        length = __builtin_amdgcn_readfirstlane(p.lengths[r]);
+    } else {
+        const DecodeShare mine(p, tid & 63, blockIdx.x, gridDim.x);
+        r = mine.r; unit = mine.unit; t0 = mine.t0; left = mine.left; share = mine.share; length = mine.length;
+        if (left <= 0) {
+            if (tid == 0) p.begun[blockIdx.x] = int4{-1, 0, 0, 0};
+            return;
         }
-        const unsigned long long found = __ballot(before + upto > wanted);
-        if (found) {
-            const int here = __builtin_ctzll(found);
-            r = r0 + here;
-            before += __shfl(upto - n, here);
-            break;
-        }
-        before += __shfl(upto, 63);
     }
-    r = __builtin_amdgcn_readfirstlane(r);
-    DecodeRequest request(p, p.lengths[r]);
-    const long long inside = at - before * p.units;      // below units * tiles of the request
-    int unit = (int)divide(inside, request.tiles);
-    int t0 = (int)(inside - (long long)unit * request.tiles);
-    unit = __builtin_amdgcn_readfirstlane(unit);
-    t0 = __builtin_amdgcn_readfirstlane(t0);
-    int left = __builtin_amdgcn_readfirstlane((int)(end - at));      // tiles of the workgroup still to do
+    DecodeRequest request(p, length);
 
-    while (left > 0) {
-        const int t1 = min(request.tiles, t0 + left);
+    do {
+        const int t1 = min(request.steps, t0 + left);      // (not DIRECT)
         const int kv_head = unit / p.head_groups, head0 = (unit - kv_head * p.head_groups) * kDecodeHeads;
         const int heads = min(kDecodeHeads, p.group - head0);
         const char* q_row = p.Q + r * p.q_request + (long long)(kv_head * p.group + head0) * p.q_head;
         u4 q[D / 32];
 #pragma unroll
-        for (int x = 0; x < D / 32; ++x) q[x] = c < heads ? *reinterpret_cast<const u4*>(q_row + c * p.q_head + x * 64 + g * 16) : u4{0, 0, 0, 0};
-        const DecodeUnit u = {p.K + kv_head * p.k_head, p.V + kv_head * p.v_head, p.table + r * p.table_stride, request.low, request.length};
+        for (int x = 0; x < D / 32; ++x)
+            q[x] = lane.c < heads ? *reinterpret_cast<const u4*>(q_row + lane.c * p.q_head + x * 64 + lane.g * 16) : u4{0, 0, 0, 0};
+        const DecodeUnit u = {p.K + kv_head * p.k_head, p.V + kv_head * p.v_head,
+                              (const __attribute__((address_space(4))) int*)(uintptr_t)(p.table + r * p.table_stride), request.low, request.length};
         DecodeState<D, BF16> state;
         state.clear();
-        for (int t = request.first + t0 + wave; t < request.first + t1; t += kDecodeWaves) {
-            DecodeTile<D> tile;
-            tile.load(p, u, t, lane);
-            state.add(p, u, q, tile, t, lane);
+        // the wavefront's tiles, those that hold a visible row
+        const int all_tiles = (request.length + kDecodeTile - 1) / kDecodeTile;
+        int tile = DIRECT ? request.low / kDecodeTile + wave : (request.first + t0) * kDecodeWaves + wave;
+        const int tiles = DIRECT ? all_tiles : min((request.first + t1) * kDecodeWaves, all_tiles);
+        if (!DIRECT && (tile + 1) * kDecodeTile <= request.low) tile += kDecodeWaves;
+        if (tile < tiles) {
+            DecodePages pages(p, u, tile);
+            do {
+                const int next = tile + WAVES;
+                const DecodePages ahead(p, u, next);      // (behind the last one the last page again)
+                state.add(p, lane, u, q, pages, tile, (LDS_PTR(char))area[wave]);
+                pages = ahead;
+                tile = next;
+            } while (tile < tiles);
         }
-        state.l += __shfl_xor(state.l, 16);
-        state.l += __shfl_xor(state.l, 32);
+        state.l = head_sum(state.l);
+        // (the lane's number made anew: what follows from it here is not to be kept in registers over the tiles)
+        const int now = lane_now(), c = now & 15, g = now >> 4;
         if (c < heads) {
             if (g == 0) {
                 m_of[wave][c] = state.m;
                 l_of[wave][c] = state.l;
             }
+            float* o = reinterpret_cast<float*>(area[wave]) + c * kPitch;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int j = 0; j < D / 16; j += 4)
-                    *reinterpret_cast<f4*>(&o_of[wave][c][(4 * g + i) * (D / 16) + j]) = f4{state.o[j][i], state.o[j + 1][i], state.o[j + 2][i], state.o[j + 3][i]};
+                    *reinterpret_cast<f4*>(o + (4 * g + i) * (D / 16) + j) = f4{state.o[j][i], state.o[j + 1][i], state.o[j + 2][i], state.o[j + 3][i]};
         }
         __syncthreads();
-        const bool whole = t0 == 0 && t1 == request.tiles;
+        const bool whole = DIRECT || (t0 == 0 && t1 == request.steps);
         const int place = 2 * blockIdx.x + (t0 == 0 ? 1 : 0);      // of a part: a unit's first part ends its workgroup's work, others begin it
-        for (int e = tid; e < heads * (D / 4); e += kDecodeThreads) {
+        for (int e = wave * 64 + now; e < heads * (D / 4); e += 64 * WAVES) {
             const int head = e / (D / 4), at4 = e % (D / 4) * 4;
             float m = m_of[0][head];
 #pragma unroll
-            for (int w = 1; w < kDecodeWaves; ++w) m = fmaxf(m, m_of[w][head]);
+            for (int w = 1; w < WAVES; ++w) m = fmaxf(m, m_of[w][head]);
             const float reference = m == -INFINITY ? 0.f : m;
             float l = 0.f;
             f4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < kDecodeWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 const float f = fast_exp2(m_of[w][head] - reference);
                 l += f * l_of[w][head];
-                o += f * *reinterpret_cast<const f4*>(&o_of[w][head][at4]);
+                o += f * *reinterpret_cast<const f4*>(reinterpret_cast<const float*>(area[w]) + head * kPitch + at4);
             }
             if (whole) {
                 const long long row = r * p.o_request + (long long)(kv_head * p.group + head0 + head) * p.o_head;
-                store_o(p.O + row + at4 * (p.o_dtype == SAWATTN_F32 ? 4 : 2), p.o_dtype, o / l);
+                store_o(p.O + row + at4 * (p.o_dtype == SAWATTN_F32 ? 4 : 2), p.o_dtype, request.length ? o / l : o);
             } else {
                 *reinterpret_cast<f4*>(p.parts + ((long long)place * p.heads_kept + head) * D + at4) = o;
                 if (at4 == 0) p.part_sums[place * p.heads_kept + head] = f2{m, l};
             }
         }
-        __syncthreads();
         left -= t1 - t0;
-        t0 = 0;
-        if (++unit == p.units && left > 0) {      // (with tiles left there is a request left that has some)
-            unit = 0;
-            do request = DecodeRequest(p, p.lengths[++r]);
-            while (request.tiles == 0);
+        if constexpr (DIRECT) return;
+        if (left <= 0) {
+            // what is missing of a unit begun here takes the workgroups behind this one, in whole shares
+            if (tid == 0)
+                p.begun[blockIdx.x] = int4{t0 == 0 && !whole ? r : -1, unit, (int)blockIdx.x + (request.steps - t1 + share - 1) / max(share, 1), 0};
+            return;
         }
-    }
+        __syncthreads();
+        t0 = 0;
+        if (++unit == p.units) {      // (with steps left there is a request left that has some)
+            unit = 0;
+            do request = DecodeRequest(p, __builtin_amdgcn_readfirstlane(p.lengths[++r]));
+            while (request.steps == 0);
+        }
+    } while (true);
 }
 
-// One workgroup per row of O: adds up the parts of rows that several workgroups shared, and clears those of empty requests.  A group of
-// D / 4 threads goes over every (1024 / D)-th part.
+// Adds up the parts of the units that several workgroups shared, a workgroup for every four heads of each, and clears the rows of empty
+// requests.  The threads that hold a head's elements, four each, go over every kGroups-th part, four parts on their way at a time.
+constexpr int kJoinThreads = 256, kJoinHeads = 2, kJoinAhead = 4;
+
 template <int D>
-__global__ __launch_bounds__(kDecodeThreads) void decode_join_kernel(DecodeParams p, int grid, int H) {
-    constexpr int kAcross = D / 4, kGroups = kDecodeThreads / kAcross;
-    __shared__ f4 o_of[kGroups][kAcross];
-    __shared__ float m_of[kGroups], l_of[kGroups];
-    const int r = blockIdx.x / H, h = blockIdx.x - r * H, tid = threadIdx.x, a = tid % kAcross, of = tid / kAcross;
-    const DecodeRequest request(p, p.lengths[r]);
-    char* const to = p.O + r * p.o_request + h * p.o_head + a * (p.o_dtype == SAWATTN_F32 ? 16 : 8);
-    if (request.tiles == 0) {
-        if (of == 0) store_o(to, p.o_dtype, f4{0.f, 0.f, 0.f, 0.f});
-        return;
-    }
-    const DecodeShares shares(p, tid & 63, grid, r);
-    const int kv_head = h / p.group, inside = h - kv_head * p.group, unit = kv_head * p.head_groups + inside / kDecodeHeads, head = inside % kDecodeHeads;
-    const long long begin = shares.before * p.units + (long long)unit * request.tiles;
-    const int w0 = (int)divide(begin, shares.share), w1 = (int)divide(begin + request.tiles - 1, shares.share);
-    if (w0 == w1) return;
+__global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(DecodeParams p, int H) {
+    constexpr int kAcross = D / 4, kGroups = kJoinThreads / (kAcross * kJoinHeads);
+    __shared__ f4 o_of[kGroups][kJoinHeads][kAcross];
+    __shared__ f2 sums_of[kGroups][kJoinHeads];
+    const int tid = threadIdx.x, a = tid % kAcross, of_head = tid / kAcross % kJoinHeads, group = tid / (kAcross * kJoinHeads);
+    const int o_size = p.o_dtype == SAWATTN_F32 ? 4 : 2;
+    const int4 unit = p.begun[blockIdx.x];
+    if (blockIdx.y == 0)
+        for (int r = blockIdx.x; r < p.R; r += gridDim.x)
+            if (p.lengths[r] <= 0)
+                for (int e = tid; e < H * kAcross; e += kJoinThreads)
+                    store_o(p.O + r * p.o_request + e / kAcross * p.o_head + e % kAcross * 4 * o_size, p.o_dtype, f4{0.f, 0.f, 0.f, 0.f});
+    if (unit.x < 0) return;
+    const int kv_head = unit.y / p.head_groups, head0 = (unit.y - kv_head * p.head_groups) * kDecodeHeads, head = blockIdx.y * kJoinHeads + of_head;
+    const bool mine = head < min(kDecodeHeads, p.group - head0);
     float m = -INFINITY, l = 0.f;
     f4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int w = w0 + of; w <= w1; w += kGroups) {
-        const long long place = (long long)(2 * w + (w == w0 ? 1 : 0)) * p.heads_kept + head;
-        const f2 sums = p.part_sums[place];
-        const f4 part = *reinterpret_cast<const f4*>(p.parts + place * D + a * 4);
-        const float next = fmaxf(m, sums[0]), reference = next == -INFINITY ? 0.f : next;
-        const float fade = fast_exp2(m - reference), f = fast_exp2(sums[0] - reference);
-        l = l * fade + sums[1] * f;
-        o = o * fade + part * f;
-        m = next;
-    }
-    o_of[of][a] = o;
-    if (a == 0) {
-        m_of[of] = m;
-        l_of[of] = l;
+    const int first = blockIdx.x, last = unit.z;
+    if (mine) {
+        for (int w = first + group; w <= last; w += kGroups * kJoinAhead) {
+            f2 sums[kJoinAhead];
+            f4 part[kJoinAhead];
+            float next = m;
+#pragma unroll
+            for (int i = 0; i < kJoinAhead; ++i) {
+                const int at = min(w + i * kGroups, last);
+                const long long place = (long long)(2 * at + (at == first ? 1 : 0)) * p.heads_kept + head;
+                sums[i] = p.part_sums[place];
+                part[i] = *reinterpret_cast<const f4*>(p.parts + place * D + a * 4);
+            }
+#pragma unroll
+            for (int i = 0; i < kJoinAhead; ++i) next = fmaxf(next, sums[i][0]);
+            const float reference = next == -INFINITY ? 0.f : next, fade = fast_exp2(m - reference);
+            l *= fade;
+            o *= fade;
+#pragma unroll
+            for (int i = 0; i < kJoinAhead; ++i)
+                if (w + i * kGroups <= last) {
+                    const float f = fast_exp2(sums[i][0] - reference);
+                    l += sums[i][1] * f;
+                    o += part[i] * f;
+                }
+            m = next;
+        }
+        o_of[group][of_head][a] = o;
+        if (a == 0) sums_of[group][of_head] = f2{m, l};
     }
     __syncthreads();
-    if (of != 0) return;
-    m = m_of[0];
+    if (group != 0 || !mine) return;
 #pragma unroll
-    for (int i = 1; i < kGroups; ++i) m = fmaxf(m, m_of[i]);
+    for (int i = 1; i < kGroups; ++i) m = fmaxf(m, sums_of[i][of_head][0]);
     const float reference = m == -INFINITY ? 0.f : m;
     l = 0.f;
     o = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kGroups; ++i) {
-        const float f = fast_exp2(m_of[i] - reference);
-        l += f * l_of[i];
-        o += f * o_of[i][a];
+        const float f = fast_exp2(sums_of[i][of_head][0] - reference);
+        l += f * sums_of[i][of_head][1];
+        o += f * o_of[i][of_head][a];
     }
-    store_o(to, p.o_dtype, o / l);
+    store_o(p.O + unit.x * p.o_request + (long long)(kv_head * p.group + head0 + head) * p.o_head + a * 4 * o_size, p.o_dtype, o / l);
 }
 
 // The launch for a problem, from what the host knows.
 struct DecodePlan {
     int group, head_groups, units, heads_kept, grid;
+    bool direct;
 };
 
-int decode_plan(const sawattn_kv_cache* cache, int R, int H, int max_pages, DecodePlan* out) {
+int decode_plan(const sawattn_kv_cache* cache, int R, int H, int max_pages, int window, DecodePlan* out) {
     if (R <= 0 || H <= 0 || max_pages <= 0) return fail(SAWATTN_ERR_INVALID_ARG, "R, H and max_pages must be positive");
     if ((long long)R * H >= (1LL << 31)) return fail(SAWATTN_ERR_INVALID_ARG, "R*H must be below 2^31");
     if (H % cache->heads) return fail(SAWATTN_ERR_INVALID_ARG, "H must be a multiple of the cache's heads");
     const long long capacity = (long long)max_pages * cache->page_size;
-    if (capacity >= (1LL << 31)) return fail(SAWATTN_ERR_INVALID_ARG, "max_pages*page_size must be below 2^31");
+    if (capacity > (1LL << 30)) return fail(SAWATTN_ERR_INVALID_ARG, "max_pages*page_size must be at most 2^30");
     out->group = H / cache->heads;
     out->head_groups = (out->group + kDecodeHeads - 1) / kDecodeHeads;
     out->units = out->head_groups * cache->heads;
     out->heads_kept = std::min(out->group, kDecodeHeads);
-    const double most = (double)R * out->units * ((capacity + kDecodeTile - 1) / kDecodeTile);      // tiles, with every table full
-    if (most >= 1e12) return fail(SAWATTN_ERR_INVALID_ARG, "R*H*max_pages*page_size is too large");
-    out->grid = (int)std::max(1.0, std::min((double)kDecodeGrid, std::ceil(most / kDecodeLeast)));
+    const long long seen = window > 0 ? std::min<long long>(capacity, window) : capacity;      // rows of a unit, with every table full
+    const double most = (double)R * out->units * ((capacity + kDecodeStep - 1) / kDecodeStep);      // steps
+    if (most >= 2147483648.0 - 2.0 * kDecodeGrid)
+        return fail(SAWATTN_ERR_INVALID_ARG, "R*H*ceil(max_pages*page_size/128) must be below 2^31 - 2048");
+    // One workgroup reads about 55 GB/s, the second kernel costs 6 us and more.  Few units: up to 500 keys at d = 128 take 8.5 us in one launch,
+    // in two 9; 1000 keys 12.5 and 9.4.  Units for every compute unit and more: 256 requests of 1000 keys, 8 heads: 170 and 190 us, 128 ragged
+    // requests up to 2000: 57 and 62.
+    const long long units = (long long)R * out->units, bytes = seen * 4 * cache->d;
+    out->direct = bytes <= (units >= kDecodeUnits ? kDecodeDirectMany : kDecodeDirectFew);
+    out->grid = out->direct ? (int)units : (int)std::min<double>(most, cache->d == 128 ? kDecodeGrid / 2 : kDecodeGrid);
     return SAWATTN_OK;
 }
 
 template <int D, bool BF16>
-int launch_decode(const DecodeParams& p, int grid, int H, hipStream_t stream) {
-    hipLaunchKernelGGL((decode_kernel<D, BF16>), dim3(grid), dim3(kDecodeThreads), 0, stream, p);
+int launch_decode(const DecodeParams& p, const DecodePlan& plan, int H, hipStream_t stream) {
+    if (plan.direct) {
+        hipLaunchKernelGGL((decode_kernel<D, BF16, kDecodeDirectWaves, true>), dim3(plan.grid), dim3(64 * kDecodeDirectWaves), 0, stream, p);
+        return launched("attn_decode");
+    }
+    hipLaunchKernelGGL((decode_kernel<D, BF16, kDecodeWaves, false>), dim3(plan.grid), dim3(64 * kDecodeWaves), 0, stream, p);
     const int rc = launched("attn_decode");
     if (rc != SAWATTN_OK) return rc;
-    hipLaunchKernelGGL((decode_join_kernel<D>), dim3(p.R * H), dim3(kDecodeThreads), 0, stream, p, grid, H);
+    hipLaunchKernelGGL((decode_join_kernel<D>), dim3(plan.grid, (plan.heads_kept + kJoinHeads - 1) / kJoinHeads), dim3(kJoinThreads), 0, stream, p, H);
     return launched("attn_decode");
 }
 
-size_t decode_bytes(const DecodePlan& plan, int d) { return (size_t)2 * plan.grid * plan.heads_kept * (d + 2) * sizeof(float); }
+size_t decode_bytes(const DecodePlan& plan, int d) { return plan.direct ? 0 : (size_t)plan.grid * (2 * plan.heads_kept * (d + 2) * sizeof(float) + sizeof(int4)); }
 
 }  // namespace sawattn
 
@@ -409,7 +523,7 @@ int attn_decode_workspace_bytes(const sawattn_kv_cache* cache, int R, int H, int
     int rc = check_cache(cache, false);
     if (rc != SAWATTN_OK) return rc;
     DecodePlan plan;
-    rc = decode_plan(cache, R, H, max_pages, &plan);
+    rc = decode_plan(cache, R, H, max_pages, 0, &plan);
     if (rc != SAWATTN_OK) return rc;
     *bytes = decode_bytes(plan, cache->d);
     return SAWATTN_OK;
@@ -422,30 +536,32 @@ int attn_decode(const void* Q, int64_t q_request, int64_t q_head, void* O, int64
     using namespace sawattn;
     int rc = check_cache(cache, true);
     if (rc != SAWATTN_OK) return rc;
+    if (window < 0) return fail(SAWATTN_ERR_INVALID_ARG, "window must not be negative");
     DecodePlan plan;
-    rc = decode_plan(cache, R, H, max_pages, &plan);
+    rc = decode_plan(cache, R, H, max_pages, window, &plan);
     if (rc != SAWATTN_OK) return rc;
-    if (!Q || !O || !table || !lengths || !workspace)
+    const size_t need = decode_bytes(plan, cache->d);
+    if (!Q || !O || !table || !lengths || (need && !workspace))
         return fail(SAWATTN_ERR_INVALID_ARG, "Q, O, table, lengths and workspace must be non-null");
+    if (cache->k_row > (1 << 26) || cache->v_row > (1 << 26)) return fail(SAWATTN_ERR_UNSUPPORTED, "cache: row strides must be at most 2^26");
     if (((uintptr_t)Q | (uintptr_t)O | (uintptr_t)workspace) & 15u)
         return fail(SAWATTN_ERR_INVALID_ARG, "Q, O and workspace must be 16-byte aligned");
     if (((uintptr_t)table | (uintptr_t)lengths) & 3u) return fail(SAWATTN_ERR_INVALID_ARG, "table and lengths must be 4-byte aligned");
     if (o_dtype != SAWATTN_F16 && o_dtype != SAWATTN_BF16 && o_dtype != SAWATTN_F32)
         return fail(SAWATTN_ERR_INVALID_ARG, "o_dtype must be SAWATTN_F16, SAWATTN_BF16 or SAWATTN_F32");
     if (!std::isfinite(scale)) return fail(SAWATTN_ERR_INVALID_ARG, "scale must be finite");
-    if (window < 0) return fail(SAWATTN_ERR_INVALID_ARG, "window must not be negative");
     if (table_stride < max_pages || (double)table_stride * R >= 1e18)
         return fail(SAWATTN_ERR_INVALID_ARG, "table_stride must be at least max_pages");
     const int d = cache->d;
     if (!good_stride(q_request, R) || !good_stride(q_head, H) || !good_stride(o_request, R) || !good_stride(o_head, H))
         return fail(SAWATTN_ERR_INVALID_ARG, "strides of Q and O must be multiples of 8, not negative");
     if ((R > 1 && o_request < d) || (H > 1 && o_head < d)) return fail(SAWATTN_ERR_INVALID_ARG, "strides of O must be at least d");
-    if (workspace_bytes < decode_bytes(plan, d))
+    if (workspace_bytes < need)
         return fail(SAWATTN_ERR_INVALID_ARG, "workspace is smaller than attn_decode_workspace_bytes reports");
     const int o_size = o_dtype == SAWATTN_F32 ? 4 : 2;
     auto extent = [](int n, int64_t stride) { return n > 1 ? (unsigned long long)(n - 1) * stride : 0ull; };
     const Range o(O, o_size * (extent(R, o_request) + extent(H, o_head) + d));
-    const Range scratch(workspace, decode_bytes(plan, d));
+    const Range scratch(workspace, need);
     const Range in[] = {
         {Q, 2 * (extent(R, q_request) + extent(H, q_head) + d)},
         {cache->k, 2 * (extent(cache->pages, cache->k_page) + extent(cache->heads, cache->k_head) + extent(cache->page_size, cache->k_row) + d)},
@@ -459,18 +575,21 @@ int attn_decode(const void* Q, int64_t q_request, int64_t q_head, void* O, int64
     p.Q = static_cast<const char*>(Q); p.q_request = 2 * q_request; p.q_head = 2 * q_head;
     p.O = static_cast<char*>(O); p.o_request = o_size * o_request; p.o_head = o_size * o_head; p.o_dtype = o_dtype;
     p.K = static_cast<const char*>(cache->k); p.V = static_cast<const char*>(cache->v);
-    p.k_page = 2 * cache->k_page; p.k_head = 2 * cache->k_head; p.k_row = 2 * cache->k_row;
-    p.v_page = 2 * cache->v_page; p.v_head = 2 * cache->v_head; p.v_row = 2 * cache->v_row;
+    p.k_page = 2 * cache->k_page; p.k_head = 2 * cache->k_head; p.k_row = (unsigned)(2 * cache->k_row);
+    p.v_page = 2 * cache->v_page; p.v_head = 2 * cache->v_head; p.v_row = (unsigned)(2 * cache->v_row);
     p.table = table; p.table_stride = table_stride; p.lengths = lengths;
-    p.parts = static_cast<float*>(workspace);
-    p.part_sums = reinterpret_cast<f2*>(p.parts + (size_t)2 * plan.grid * plan.heads_kept * d);
+    if (need) {
+        p.parts = static_cast<float*>(workspace);
+        p.begun = reinterpret_cast<int4*>(p.parts + (size_t)2 * plan.grid * plan.heads_kept * d);
+        p.part_sums = reinterpret_cast<f2*>(p.begun + plan.grid);
+    }
     p.c = (float)((double)scale * 1.4426950408889634074);
     p.R = R; p.capacity = max_pages * cache->page_size; p.window = window; p.pages = cache->pages; p.shift = page_shift(cache->page_size);
     p.group = plan.group; p.head_groups = plan.head_groups; p.units = plan.units; p.heads_kept = plan.heads_kept;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const bool bf = cache->dtype == SAWATTN_BF16;
-    if (d == 128) return bf ? launch_decode<128, true>(p, plan.grid, H, stream) : launch_decode<128, false>(p, plan.grid, H, stream);
-    return bf ? launch_decode<64, true>(p, plan.grid, H, stream) : launch_decode<64, false>(p, plan.grid, H, stream);
+    if (d == 128) return bf ? launch_decode<128, true>(p, plan, H, stream) : launch_decode<128, false>(p, plan, H, stream);
+    return bf ? launch_decode<64, true>(p, plan, H, stream) : launch_decode<64, false>(p, plan, H, stream);
 }
 
 }  // extern "C"

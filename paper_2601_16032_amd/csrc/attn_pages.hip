@@ -166,7 +166,7 @@ extern "C" int attn_kv_pages(const int32_t* lengths, const int32_t* new_tokens, 
     if (R <= 0 || max_pages <= 0 || ring <= 0 || tokens < 0)
         return fail(SAWATTN_ERR_INVALID_ARG, "R, max_pages and ring must be positive, tokens not negative");
     if (R > SAWATTN_MOST_REQUESTS) return fail(SAWATTN_ERR_UNSUPPORTED, "more requests than SAWATTN_MOST_REQUESTS");
-    if (page_shift(page_size) < 0) return fail(SAWATTN_ERR_UNSUPPORTED, "page size must be a power of two from 8 to 2^20");
+    if (page_shift(page_size) < 0) return fail(SAWATTN_ERR_UNSUPPORTED, "page size must be a power of two from 16 to 2^20");
     if ((long long)R * max_pages >= (1LL << 31) || (long long)max_pages * page_size >= (1LL << 31) ||
         tokens >= (1LL << 31) - (1 << 20))
         return fail(SAWATTN_ERR_INVALID_ARG, "R*max_pages and max_pages*page_size must be below 2^31, tokens below 2^31 - 2^20");

@@ -3,9 +3,9 @@
 
 namespace sawattn {
 
-// log2 of a page size, or -1 where it is none: a power of two from 8 (the attention reads eight rows of a page at a time) to 2^20.
+// log2 of a page size, or -1 where it is none: a power of two from 16 (the attention reads sixteen rows of a page at a time) to 2^20.
 inline int page_shift(int page_size) {
-    if (page_size < 8 || page_size > (1 << 20) || (page_size & (page_size - 1))) return -1;
+    if (page_size < 16 || page_size > (1 << 20) || (page_size & (page_size - 1))) return -1;
     return __builtin_ctz((unsigned)page_size);
 }
 
@@ -24,7 +24,7 @@ inline int check_cache(const sawattn_kv_cache* c, bool pointers) {
     if (!c) return fail(SAWATTN_ERR_INVALID_ARG, "cache must be non-null");
     if (c->pages <= 0 || c->heads <= 0) return fail(SAWATTN_ERR_INVALID_ARG, "cache: pages and heads must be positive");
     if (c->d != 64 && c->d != 128) return fail(SAWATTN_ERR_UNSUPPORTED, "head dimension must be 64 or 128");
-    if (page_shift(c->page_size) < 0) return fail(SAWATTN_ERR_UNSUPPORTED, "page size must be a power of two from 8 to 2^20");
+    if (page_shift(c->page_size) < 0) return fail(SAWATTN_ERR_UNSUPPORTED, "page size must be a power of two from 16 to 2^20");
     if (c->dtype != SAWATTN_F16 && c->dtype != SAWATTN_BF16)
         return fail(SAWATTN_ERR_INVALID_ARG, "cache: dtype must be SAWATTN_F16 or SAWATTN_BF16");
     if (!pointers) return SAWATTN_OK;

@@ -50,10 +50,10 @@ def test_pages_refusals():
     refused(call(tokens=-1), bad, "not negative")
     refused(call(tokens=2 ** 31 - 2 ** 20), bad, "below")
     refused(call(R=4097), no, "SAWATTN_MOST_REQUESTS")
-    for ps in (0, 4, 24, 2 ** 21, -16):
+    for ps in (0, 8, 24, 2 ** 21, -16):
         refused(call(ps=ps), no, "page size")
     refused(call(wide=2 ** 27, stride=2 ** 27), bad, "below 2^31")
-    refused(call(R=4096, wide=2 ** 19, stride=2 ** 19, ps=8), bad, "below 2^31")
+    refused(call(R=4096, wide=2 ** 19, stride=2 ** 19, ps=16), bad, "below 2^31")
     refused(call(stride=7), bad, "table_stride")
     refused(call(out=base["lengths"]), bad, "overlaps an input")
     refused(call(state_out=base["state"] + 4), bad, "overlaps an input")
@@ -69,7 +69,7 @@ def cache_struct(**kw):
 
 
 BAD_CACHES = [(dict(k=None), 1, "non-null"), (dict(v=0x20000008), 1, "aligned"), (dict(pages=0), 1, "positive"), (dict(heads=-1), 1, "positive"),
-              (dict(d=96), 2, "head dimension"), (dict(page_size=24), 2, "page size"), (dict(page_size=4), 2, "page size"),
+              (dict(d=96), 2, "head dimension"), (dict(page_size=24), 2, "page size"), (dict(page_size=8), 2, "page size"),
               (dict(dtype=2), 1, "dtype"), (dict(k_row=100), 1, "row strides"), (dict(v_page=-8), 1, "page strides"),
               (dict(v_head=4), 1, "head strides"), (dict(k_page=2 ** 60), 1, "page strides")]
 
@@ -120,9 +120,10 @@ def test_decode_refusals():
     L = binding.lib()
     cache = cache_struct()
     n = ctypes.c_size_t(0)
-    assert L.attn_decode_workspace_bytes(ctypes.addressof(cache), 3, 8, 10, ctypes.byref(n)) == 0 and n.value > 0
+    assert L.attn_decode_workspace_bytes(ctypes.addressof(cache), 3, 8, 10, ctypes.byref(n)) == 0 and n.value == 0      # short tables
+    assert L.attn_decode_workspace_bytes(ctypes.addressof(cache), 3, 8, 100, ctypes.byref(n)) == 0 and n.value > 0
     base = dict(Q=0x1000000, qr=1024, qh=128, O=0x2000000, orow=1024, oh=128, odt=0, cache=ctypes.addressof(cache), table=0x3000000,
-                stride=10, wide=10, lengths=0x4000000, R=3, H=8, scale=0.1, window=0, ws=0x5000000, bytes=n.value)
+                stride=100, wide=100, lengths=0x4000000, R=3, H=8, scale=0.1, window=0, ws=0x5000000, bytes=n.value)
 
     def call(**kw):
         return L.attn_decode(*dict(base, **kw).values(), None)
@@ -135,12 +136,13 @@ def test_decode_refusals():
         refused(call(**{name: 0}), bad, "positive")
     refused(call(H=7), bad, "multiple of the cache's heads")
     refused(call(R=2 ** 28, H=8), bad, "R*H")
-    refused(call(wide=2 ** 27, stride=2 ** 27), bad, "below 2^31")
+    refused(call(wide=2 ** 27, stride=2 ** 27), bad, "at most 2^30")
+    refused(call(R=2 ** 20, wide=2 ** 16, stride=2 ** 16), bad, "2^31 - 2048")
     refused(call(odt=3), bad, "o_dtype")
     for scale in (math.nan, math.inf):
         refused(call(scale=scale), bad, "scale")
     refused(call(window=-1), bad, "window")
-    refused(call(stride=9), bad, "table_stride")
+    refused(call(stride=99), bad, "table_stride")
     for name, value in (("qr", -8), ("qh", 100), ("orow", 1020), ("oh", -128)):
         refused(call(**{name: value}), bad, "strides of Q and O")
     refused(call(oh=64), bad, "at least d")
@@ -218,7 +220,7 @@ def check_pages(*case, stride=0):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("R,ps,most,most_new", [(1, 16, 0, 1), (1, 8, 7, 1), (1, 16, 16, 5000), (2, 64, 100, 1), (63, 16, 40, 1), (64, 8, 9, 30),
+@pytest.mark.parametrize("R,ps,most,most_new", [(1, 16, 0, 1), (1, 16, 7, 1), (1, 16, 16, 5000), (2, 64, 100, 1), (63, 16, 40, 1), (64, 16, 9, 30),
                                                 (65, 1024, 3000, 700), (257, 16, 600, 1), (1000, 32, 900, 40), (4096, 16, 64, 3)])
 @pytest.mark.parametrize("pool", ["enough", "exact", "half", "none"])
 def test_pages(R, ps, most, most_new, pool):
@@ -233,8 +235,8 @@ def test_pages_refuses_requests_not_calls():
     check_pages(*pages_case(rng, 90, 16, 200, 100, room=1))
     check_pages(*pages_case(rng, 90, 16, 200, 100, tokens=lambda total: total // 2))
     check_pages(*pages_case(rng, 90, 16, 200, 100, tokens=lambda total: 0))
-    check_pages(*pages_case(rng, 300, 8, 500, 1, ends=1.1))
-    check_pages(*pages_case(rng, 300, 8, 500, 1, ends=0, idle=1.1))
+    check_pages(*pages_case(rng, 300, 16, 500, 1, ends=1.1))
+    check_pages(*pages_case(rng, 300, 16, 500, 1, ends=0, idle=1.1))
 
 
 @pytest.mark.gpu
@@ -304,7 +306,7 @@ def test_prepare_rows(d, rot, dtype, interleaved, norm):
 @pytest.mark.parametrize("page_first", [False, True])
 def test_prepare_fills_the_cache(dtype, d, page_first):
     """Rows go to their slots and nowhere else; padding and slots outside the cache are left out; the copies for attn_fwd are the same rows."""
-    B, N, H, KH, ps, pages = 2, 21, 6, 3, 8, 9
+    B, N, H, KH, ps, pages = 2, 21, 6, 3, 16, 5
     q, k, v, (wq, wk) = prepare_inputs(B, N, H, KH, d, dtype, seed=3)
     rng = np.random.default_rng(8)
     pos, slots = rng.integers(0, 5000, (B, N)), rng.permutation(pages * ps)[:B * N].reshape(B, N)
@@ -428,7 +430,7 @@ LENGTHS = [0, 1, 7, 8, 9, 31, 32, 33, 63, 64, 65, 127, 129, 255, 257, 1000, 0, 1
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("G,KH", [(1, 1), (1, 5), (3, 2), (4, 2), (8, 1), (16, 1), (17, 1), (40, 2)])
 def test_decode(d, dtype, G, KH):
-    ps = {1: 8, 3: 16, 4: 32, 8: 64, 16: 1024, 17: 16, 40: 128}[G]
+    ps = {1: 16, 3: 16, 4: 32, 8: 64, 16: 1024, 17: 16, 40: 128}[G]
     cache, table, keys = fill_cache(LENGTHS, KH, d, ps, dtype, seed=G * d, page_first=G == 4)
     q = queries(len(LENGTHS), G * KH, d, dtype, seed=1)
     lengths = torch.tensor(LENGTHS, dtype=torch.int32, device="cuda")
@@ -562,7 +564,7 @@ def test_decode_far_into_a_large_cache():
 class Server:
     """A few requests of one layer, stepped as a program would: tables, preparation, attention; and the same on the host in 64 bits."""
 
-    def __init__(self, R=6, H=6, KH=2, d=64, ps=8, wide=12, dtype="bf16", seed=1):
+    def __init__(self, R=6, H=6, KH=2, d=64, ps=16, wide=12, dtype="bf16", seed=1):
         self.R, self.H, self.KH, self.d, self.ps, self.dtype = R, H, KH, d, ps, dtype
         i32 = {"dtype": torch.int32, "device": "cuda"}
         pages = R * wide
