@@ -323,6 +323,13 @@ typedef struct sawattn_rows {
     int64_t sequence, token, head;      /* strides in elements: not negative, multiples of 8 */
 } sawattn_rows;
 
+/* What attn_qkv_prepare reads and writes. */
+typedef struct sawattn_qkv {
+    sawattn_rows q, k, v;               /* read */
+    sawattn_rows q_out;                 /* written.  May be q itself (same data and strides) */
+    sawattn_rows k_out, v_out;          /* written, or data NULL in both.  May be k and v themselves */
+} sawattn_qkv;
+
 #define SAWATTN_MOST_REQUESTS 4096      /* requests per call of attn_kv_pages */
 #define SAWATTN_REQUEST_ENDS (-1)       /* in new_tokens: the request's pages go back to the free list */
 
@@ -365,10 +372,8 @@ int attn_kv_pages(const int32_t* lengths, const int32_t* new_tokens, int R, int3
  * Q and K becomes x / sqrt(mean(x^2) + eps) * weight, the pairs of its first `rotated` elements are turned by
  * position * frequencies[i], and the result is written where the attention reads it.  V is copied.
  *
- *   q, k, v            host structs, read during the call; the rows on the device, read: [B, N] tokens of H, KH and KH heads
- *   q_out              rows of Q, written.  May be q itself (same data and strides).
- *   k_out, v_out       rows of K and V, written, or NULL.  May be k and v themselves.  With the strides of [B, H, N, d] these three are
- *                      the inputs of attn_fwd.
+ *   rows               host struct, read during the call: [B, N] tokens of H (q, q_out) or KH heads.  With the strides of [B, H, N, d] the
+ *                      outputs are the inputs of attn_fwd.
  *   cache, slots       both or neither NULL: row t = b*N + n of K and V is also written to slot slots[t] (device, int64 [B*N]) of
  *                      the cache; slots outside 0 .. pages*page_size - 1 are not written.  No slot may appear twice.
  *   positions          device, read: int32 [B*N].  A token of negative position is padding: nothing of it is read or written.
@@ -382,11 +387,9 @@ int attn_kv_pages(const int32_t* lengths, const int32_t* new_tokens, int R, int3
  * Other overlaps of outputs with inputs or with each other are not allowed (and not looked for).  Angles are reduced in 64 bits, all
  * else is computed in 32 and rounded once.  One launch; no workspace.  Stream and errors as attn_fwd.
  */
-int attn_qkv_prepare(const sawattn_rows* q, const sawattn_rows* k, const sawattn_rows* v, const sawattn_rows* q_out,
-                     const sawattn_rows* k_out, const sawattn_rows* v_out, const sawattn_kv_cache* cache,
-                     const int64_t* slots, const int32_t* positions, const float* q_weight, const float* k_weight, float eps,
-                     const double* frequencies, int rotated, int interleaved, int B, int N, int H, int KH, int d, int dtype,
-                     void* hip_stream);
+int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache* cache, const int64_t* slots, const int32_t* positions,
+                     const float* q_weight, const float* k_weight, float eps, const double* frequencies, int rotated,
+                     int interleaved, int B, int N, int H, int KH, int d, int dtype, void* hip_stream);
 
 /*
  * attn_decode -- attention of one new token per request over its pages: O[r][h] = softmax(q . K^T * scale) V over the last

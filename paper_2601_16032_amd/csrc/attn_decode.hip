@@ -70,17 +70,6 @@ struct DecodeRequest {
     }
 };
 
-// Sum over the lanes up to and including this one.
-__device__ __forceinline__ int lanes_upto(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);      // row_shr 1, 2, 4, 8: within rows of 16
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // the last lane of rows 0 and 2 into rows 1 and 3
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // lane 31 into rows 2 and 3
-    return x;
-}
-
 // How the steps are dealt out, from the lengths alone: what workgroup `wg` of `grid` has to do.  Every wavefront works it out for itself.
 struct DecodeShare {
     int share;                 // steps of a workgroup

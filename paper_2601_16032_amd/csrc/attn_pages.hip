@@ -5,12 +5,10 @@
 // and T_r <= tokens of the batch.  P and T never fall, so what is left over is a tail of the requests that need pages, and the pages
 // taken are the largest P_r granted.  Token t belongs to the first r with T_r > t; its row is length_r + t - T_(r-1).
 //
-// Every workgroup makes the sums for itself (4096 requests at most: 16 of a thread, one scan over the threads; from the L2) and then takes
+// Every workgroup makes the sums for itself (4096 requests at most, 4 of a thread, one scan over the threads; from the L2) and then takes
 // its share of the tokens, each found by bisection in LDS: one launch, no workspace, nothing to wait for.  The pages need no loop of their own:
 // every new page has exactly one token whose row is its first, and that token enters it into the table.
 namespace sawattn {
-
-constexpr int kPagesThreads = 256;
 
 struct PagesParams {
     const int* lengths;
@@ -51,30 +49,27 @@ struct PageRequest {
     __device__ __forceinline__ PageSums sums() const { return {(long long)max(added, 0), missing, back}; }
 };
 
-__global__ __launch_bounds__(kPagesThreads) void kv_pages_kernel(PagesParams p) {
+// THREADS: 256, or 1024 for more than 1024 requests, so that four are left to a thread at most (4096 requests: 16.8 -> 10.3 us; but 257: 4.2 -> 4.6).
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void kv_pages_kernel(PagesParams p) {
     __shared__ int tokens_upto[SAWATTN_MOST_REQUESTS];      // T_r
     __shared__ int back_upto[SAWATTN_MOST_REQUESTS];        // Q_r
     __shared__ int first_page[SAWATTN_MOST_REQUESTS];       // P_(r-1): its first new page, counted from the ring's first; -1: nothing granted
-    __shared__ PageSums of_wave[kPagesThreads / 64];
-    __shared__ int taken_by_wave[kPagesThreads / 64];
+    __shared__ PageSums of_wave[THREADS / 64];
+    __shared__ int taken_by_wave[THREADS / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const unsigned F = (unsigned)p.ring_size;
     const int first_given = p.state[0], free_given = p.state[1];
-    const int each = (p.R + kPagesThreads - 1) / kPagesThreads, r0 = tid * each, r1 = min(p.R, r0 + each);
+    const int each = (p.R + THREADS - 1) / THREADS, r0 = tid * each, r1 = min(p.R, r0 + each);
 
     PageSums mine = {0, 0, 0};
     for (int r = r0; r < r1; ++r) mine.add(PageRequest(p, r).sums());
-    PageSums upto = mine;
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2) {
-        const PageSums o = {__shfl_up(upto.tokens, step), __shfl_up(upto.missing, step), __shfl_up(upto.back, step)};
-        if (lane >= step) upto.add(o);
-    }
+    const PageSums upto = {lanes_upto(mine.tokens), lanes_upto(mine.missing), lanes_upto(mine.back)};
     if (lane == 63) of_wave[wave] = upto;
     __syncthreads();
     PageSums before = {upto.tokens - mine.tokens, upto.missing - mine.missing, upto.back - mine.back}, all = {0, 0, 0};
 #pragma unroll
-    for (int w = 0; w < kPagesThreads / 64; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         if (w < wave) before.add(of_wave[w]);
         all.add(of_wave[w]);
     }
@@ -108,15 +103,15 @@ __global__ __launch_bounds__(kPagesThreads) void kv_pages_kernel(PagesParams p) 
     }
     __syncthreads();
     if (blockIdx.x == 0 && tid == 0) {
-        for (int w = 0; w < kPagesThreads / 64; ++w) taken = max(taken, taken_by_wave[w]);
+        for (int w = 0; w < THREADS / 64; ++w) taken = max(taken, taken_by_wave[w]);
         p.offsets[0] = 0;
         p.state_out[0] = (int)(((unsigned long long)first + (unsigned)taken) % F);
         p.state_out[1] = min(available - taken + all.back, p.ring_size);
     }
 
-    const int stride = gridDim.x * kPagesThreads;
+    const int stride = gridDim.x * THREADS;
     const int filled = (int)min(all.tokens, (long long)p.tokens);
-    for (int t = blockIdx.x * kPagesThreads + tid; t < p.tokens; t += stride) {
+    for (int t = blockIdx.x * THREADS + tid; t < p.tokens; t += stride) {
         long long slot = -1;
         int row = -1;
         if (t < filled) {
@@ -145,7 +140,7 @@ __global__ __launch_bounds__(kPagesThreads) void kv_pages_kernel(PagesParams p) 
         p.slots[t] = slot;
         p.positions[t] = row;
     }
-    for (int e = blockIdx.x * kPagesThreads + tid; e < all.back; e += stride) {      // pages given back, behind the last free one
+    for (int e = blockIdx.x * THREADS + tid; e < all.back; e += stride) {      // pages given back, behind the last free one
         int low = 0, high = p.R - 1;
         while (low < high) {
             const int mid = (low + high) >> 1;
@@ -193,8 +188,9 @@ extern "C" int attn_kv_pages(const int32_t* lengths, const int32_t* new_tokens, 
     }
     PagesParams p = {lengths, new_tokens, table, table_stride, free_pages, free_state, lengths_out, granted, token_offsets,
                      free_state_out, reinterpret_cast<long long*>(slots), positions, R, max_pages, page_shift(page_size), ring, tokens};
-    // Two tokens per thread; a workgroup for every 64 requests at least, whose pages it may have to give back.
-    const int grid = std::min(256, std::max((tokens + 2 * kPagesThreads - 1) / (2 * kPagesThreads), (R + 63) / 64));
-    hipLaunchKernelGGL(kv_pages_kernel, dim3(grid), dim3(kPagesThreads), 0, static_cast<hipStream_t>(hip_stream), p);
+    // 512 tokens to a workgroup, and a workgroup for every 64 requests at least, whose pages it may have to give back.
+    const int grid = std::min(256, std::max((tokens + 511) / 512, (R + 63) / 64));
+    if (R <= 1024) hipLaunchKernelGGL((kv_pages_kernel<256>), dim3(grid), dim3(256), 0, static_cast<hipStream_t>(hip_stream), p);
+    else hipLaunchKernelGGL((kv_pages_kernel<1024>), dim3(grid), dim3(1024), 0, static_cast<hipStream_t>(hip_stream), p);
     return launched("attn_kv_pages");
 }

@@ -12,7 +12,6 @@
 namespace sawattn {
 
 constexpr int kPrepareThreads = 256;
-constexpr int kPrepareBatch = 4;      // rows of a lane in flight
 
 struct Rows {
     char* data;
@@ -32,7 +31,7 @@ struct PrepareParams {
     const float* k_weight;
     const double* frequencies;
     float eps;
-    int rotated, tokens, N, H, KH, batches, chunks;      // of a token's rows a wavefront takes `batches` batches; `chunks` wavefronts take all
+    int rotated, tokens, N, H, KH, trips, chunks;      // a wavefront takes a token's rows in `trips` trips, `chunks` wavefronts take all
 };
 
 // x added up over the aligned group of LANES (8 or 16) lanes, in every lane.
@@ -115,72 +114,64 @@ __global__ __launch_bounds__(kPrepareThreads) void qkv_prepare_kernel(PreparePar
     char* const v_slot = page >= 0 ? p.cache_v + page * p.v_page + page_row * p.v_row : nullptr;
 
     const int rows = p.H + 2 * p.KH;
-    for (int batch = 0; batch < p.batches; ++batch) {
-        const int row0 = (chunk * p.batches + batch) * (kRows * kPrepareBatch) + group;
-        if (row0 - group >= rows) break;
-        u2 x[kPrepareBatch][2];
-#pragma unroll
-        for (int i = 0; i < kPrepareBatch; ++i) {
-            const int row = row0 + i * kRows;
-            if (row >= rows) continue;
-            const char* from = row < p.H ? q + row * p.q.head : row < p.H + p.KH ? k + (row - p.H) * p.k.head : v + (row - p.H - p.KH) * p.v.head;
-            if constexpr (INTERLEAVED) {
-                const u4 both = *reinterpret_cast<const u4*>(from + low);
-                x[i][0] = u2{both[0], both[1]};
-                x[i][1] = u2{both[2], both[3]};
-            } else {
-                x[i][0] = *reinterpret_cast<const u2*>(from + low);
-                x[i][1] = *reinterpret_cast<const u2*>(from + high);
-            }
+    for (int trip = 0; trip < p.trips; ++trip) {
+        const int row = (chunk * p.trips + trip) * kRows + group;
+        if (row >= rows) break;
+        const bool is_q = row < p.H, is_v = row >= p.H + p.KH;
+        const int head = is_q ? row : is_v ? row - p.H - p.KH : row - p.H;
+        const char* from = is_q ? q + head * p.q.head : is_v ? v + head * p.v.head : k + head * p.k.head;
+        u2 x[2];
+        if constexpr (INTERLEAVED) {
+            const u4* at = reinterpret_cast<const u4*>(from + low);
+            const u4 both = *at;
+            x[0] = u2{both[0], both[1]};
+            x[1] = u2{both[2], both[3]};
+        } else {
+            const u2* at = reinterpret_cast<const u2*>(from + low);
+            const u2* and_at = reinterpret_cast<const u2*>(from + high);
+            x[0] = *at;
+            x[1] = *and_at;
         }
+        if (!is_v) {
+            float y[8];
 #pragma unroll
-        for (int i = 0; i < kPrepareBatch; ++i) {
-            const int row = row0 + i * kRows;
-            if (row >= rows) continue;
-            const bool is_q = row < p.H, is_v = row >= p.H + p.KH;
-            if (!is_v) {
-                float y[8];
+            for (int e = 0; e < 8; ++e) y[e] = widen<BF16>(x[e / 4][e / 2 % 2], e % 2);
+            if (is_q ? p.q_weight != nullptr : p.k_weight != nullptr) {
+                float square = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = widen<BF16>(x[i][e / 4][e / 2 % 2], e % 2);
-                if (is_q ? p.q_weight != nullptr : p.k_weight != nullptr) {
-                    float square = 0.f;
+                for (int e = 0; e < 8; ++e) square += y[e] * y[e];
+                const float norm = 1.f / sqrtf(group_sum<kLanes>(square) * (1.f / D) + p.eps);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) square += y[e] * y[e];
-                    const float norm = 1.f / sqrtf(group_sum<kLanes>(square) * (1.f / D) + p.eps);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] *= norm * (is_q ? wq[e / 4][e % 4] : wk[e / 4][e % 4]);
-                }
-                if (turns) {
-#pragma unroll
-                    for (int i2 = 0; i2 < 4; ++i2) {
-                        const int ea = INTERLEAVED ? 2 * i2 : i2, eb = INTERLEAVED ? 2 * i2 + 1 : i2 + 4;
-                        const float a = y[ea], c = y[eb];
-                        y[ea] = a * cosine[i2] - c * sine[i2];
-                        y[eb] = a * sine[i2] + c * cosine[i2];
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) x[i][e / 4][e / 2 % 2] = narrow<BF16>(y[e], y[e + 1]);
+                for (int e = 0; e < 8; ++e) y[e] *= norm * (is_q ? wq[e / 4][e % 4] : wk[e / 4][e % 4]);
             }
-            auto put = [&](char* to) {
-                if constexpr (INTERLEAVED) {
-                    *reinterpret_cast<u4*>(to + low) = u4{x[i][0][0], x[i][0][1], x[i][1][0], x[i][1][1]};
-                } else {
-                    *reinterpret_cast<u2*>(to + low) = x[i][0];
-                    *reinterpret_cast<u2*>(to + high) = x[i][1];
+            if (turns) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int ea = INTERLEAVED ? 2 * i : i, eb = INTERLEAVED ? 2 * i + 1 : i + 4;
+                    const float a = y[ea], c = y[eb];
+                    y[ea] = a * cosine[i] - c * sine[i];
+                    y[eb] = a * sine[i] + c * cosine[i];
                 }
-            };
-            if (is_q) {
-                put(q_out + row * p.q_out.head);
-            } else if (!is_v) {
-                const int head = row - p.H;
-                if (k_out) put(k_out + head * p.k_out.head);
-                if (k_slot) put(k_slot + head * p.k_head);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) x[e / 4][e / 2 % 2] = narrow<BF16>(y[e], y[e + 1]);
+        }
+        auto put = [&](char* to) {
+            if constexpr (INTERLEAVED) {
+                __builtin_nontemporal_store(u4{x[0][0], x[0][1], x[1][0], x[1][1]}, reinterpret_cast<u4*>(to + low));
             } else {
-                const int head = row - p.H - p.KH;
-                if (v_out) put(v_out + head * p.v_out.head);
-                if (v_slot) put(v_slot + head * p.v_head);
+                __builtin_nontemporal_store(x[0], reinterpret_cast<u2*>(to + low));
+                __builtin_nontemporal_store(x[1], reinterpret_cast<u2*>(to + high));
             }
+        };
+        if (is_q) {
+            put(q_out + head * p.q_out.head);
+        } else if (!is_v) {
+            if (k_out) put(k_out + head * p.k_out.head);
+            if (k_slot) put(k_slot + head * p.k_head);
+        } else {
+            if (v_out) put(v_out + head * p.v_out.head);
+            if (v_slot) put(v_slot + head * p.v_head);
         }
     }
 }
@@ -193,11 +184,9 @@ void launch_prepare(const PrepareParams& p, bool interleaved, int grid, hipStrea
 
 }  // namespace sawattn
 
-extern "C" int attn_qkv_prepare(const sawattn_rows* q, const sawattn_rows* k, const sawattn_rows* v, const sawattn_rows* q_out,
-                                const sawattn_rows* k_out, const sawattn_rows* v_out, const sawattn_kv_cache* cache,
-                                const int64_t* slots, const int32_t* positions, const float* q_weight, const float* k_weight,
-                                float eps, const double* frequencies, int rotated, int interleaved, int B, int N, int H, int KH,
-                                int d, int dtype, void* hip_stream) {
+extern "C" int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache* cache, const int64_t* slots, const int32_t* positions,
+                                const float* q_weight, const float* k_weight, float eps, const double* frequencies, int rotated,
+                                int interleaved, int B, int N, int H, int KH, int d, int dtype, void* hip_stream) {
     using namespace sawattn;
     if (B <= 0 || N <= 0 || H <= 0 || KH <= 0 || d <= 0) return fail(SAWATTN_ERR_INVALID_ARG, "B, N, H, KH and d must be positive");
     if (d != 64 && d != 128) return fail(SAWATTN_ERR_UNSUPPORTED, "head dimension must be 64 or 128");
@@ -207,9 +196,9 @@ extern "C" int attn_qkv_prepare(const sawattn_rows* q, const sawattn_rows* k, co
         return fail(SAWATTN_ERR_INVALID_ARG, "B*N must be below 2^31 and H + 2*KH at most 2^16");
     if (rotated < 0 || rotated > d || rotated % 8) return fail(SAWATTN_ERR_INVALID_ARG, "rotated must be a multiple of 8 from 0 to d");
     if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(SAWATTN_ERR_INVALID_ARG, "eps must be finite and not negative");
-    if (!q || !k || !v || !q_out || !positions || (rotated && !frequencies))
+    if (!rows || !rows->q.data || !rows->k.data || !rows->v.data || !rows->q_out.data || !positions || (rotated && !frequencies))
         return fail(SAWATTN_ERR_INVALID_ARG, "q, k, v, q_out, positions and (with rotated > 0) frequencies must be non-null");
-    if ((k_out == nullptr) != (v_out == nullptr)) return fail(SAWATTN_ERR_INVALID_ARG, "k_out and v_out must be given together");
+    if ((rows->k_out.data == nullptr) != (rows->v_out.data == nullptr)) return fail(SAWATTN_ERR_INVALID_ARG, "k_out and v_out must be given together");
     if ((cache == nullptr) != (slots == nullptr)) return fail(SAWATTN_ERR_INVALID_ARG, "cache and slots must be given together");
     if (((uintptr_t)q_weight | (uintptr_t)k_weight | (uintptr_t)frequencies) & 15u)
         return fail(SAWATTN_ERR_INVALID_ARG, "q_weight, k_weight and frequencies must be 16-byte aligned");
@@ -217,11 +206,11 @@ extern "C" int attn_qkv_prepare(const sawattn_rows* q, const sawattn_rows* k, co
         return fail(SAWATTN_ERR_INVALID_ARG, "positions and slots must be aligned to their elements");
     PrepareParams p{};
     const struct { const sawattn_rows* from; Rows* to; int heads; } tensors[] = {
-        {q, &p.q, H}, {k, &p.k, KH}, {v, &p.v, KH}, {q_out, &p.q_out, H}, {k_out, &p.k_out, KH}, {v_out, &p.v_out, KH}};
+        {&rows->q, &p.q, H}, {&rows->k, &p.k, KH}, {&rows->v, &p.v, KH}, {&rows->q_out, &p.q_out, H}, {&rows->k_out, &p.k_out, KH}, {&rows->v_out, &p.v_out, KH}};
     for (int i = 0; i < 6; ++i) {
         const sawattn_rows* s = tensors[i].from;
-        if (!s) continue;
-        if (!s->data || ((uintptr_t)s->data & 15u)) return fail(SAWATTN_ERR_INVALID_ARG, "rows must be non-null and 16-byte aligned");
+        if (!s->data) continue;
+        if ((uintptr_t)s->data & 15u) return fail(SAWATTN_ERR_INVALID_ARG, "rows must be 16-byte aligned");
         if (!good_stride(s->sequence, B) || !good_stride(s->token, N) || !good_stride(s->head, tensors[i].heads))
             return fail(SAWATTN_ERR_INVALID_ARG, "strides of rows must be multiples of 8, not negative");
         // rows written must be rows of their own
@@ -248,11 +237,13 @@ extern "C" int attn_qkv_prepare(const sawattn_rows* q, const sawattn_rows* k, co
     p.positions = positions;
     p.q_weight = q_weight; p.k_weight = k_weight; p.frequencies = frequencies;
     p.eps = eps; p.rotated = rotated; p.tokens = B * N; p.N = N; p.H = H; p.KH = KH;
-    // A wavefront takes all rows of a token, or, where that would leave compute units without work, fewer: down to one batch.
-    const int rows = H + 2 * KH, per_batch = kPrepareBatch * 64 / (d / 8), all = (rows + per_batch - 1) / per_batch;
-    const int wanted = (int)std::min<long long>(all, (2048 + p.tokens - 1) / p.tokens);
-    p.batches = (all + wanted - 1) / wanted;
-    p.chunks = (all + p.batches - 1) / p.batches;
+    // A wavefront takes all rows of a token, or, where that would make fewer than 4096 wavefronts, fewer of them, 4 (d = 128) or 8 at least.  Measured, 32 +
+    // 2 x 8 heads of 128 into the cache, 2048, 4096, 8192 and 65536 wavefronts: 1024 tokens 9.0, 8.7, 9.7, 10.9 us; 4096 tokens 28.0, 28.2, 28.3, 39.5;
+    // 2048 tokens 14.8, 12.8, 13.7, 19.0.
+    const int heads = H + 2 * KH, at_once = 64 / (d / 8), all = (heads + at_once - 1) / at_once;
+    const int wanted = (int)std::min<long long>(all, (4096 + p.tokens - 1) / p.tokens);
+    p.trips = (all + wanted - 1) / wanted;
+    p.chunks = (all + p.trips - 1) / p.trips;
     const long long waves = (long long)p.tokens * p.chunks;
     if (waves >= (1LL << 31) - kPrepareThreads / 64) return fail(SAWATTN_ERR_INVALID_ARG, "too many tokens");
     const int grid = (int)((waves + kPrepareThreads / 64 - 1) / (kPrepareThreads / 64));

@@ -1,7 +1,26 @@
-// What the operators over a paged key-value cache share: checks on the host.
+// What the operators over a paged key-value cache share: sums over lanes, and checks on the host.
 #pragma once
 
 namespace sawattn {
+
+// Sum over the lanes up to and including this one.
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ int from_lane(int x) { return __builtin_amdgcn_update_dpp(0, x, CONTROL, ROWS, 0xf, false); }
+template <int CONTROL, int ROWS>
+__device__ __forceinline__ long long from_lane(long long x) {
+    const unsigned low = from_lane<CONTROL, ROWS>((int)x), high = from_lane<CONTROL, ROWS>((int)(x >> 32));
+    return (long long)((unsigned long long)high << 32 | low);
+}
+template <typename T>
+__device__ __forceinline__ T lanes_upto(T x) {
+    x += from_lane<0x111, 0xf>(x);      // row_shr 1, 2, 4, 8: within rows of 16 lanes
+    x += from_lane<0x112, 0xf>(x);
+    x += from_lane<0x114, 0xf>(x);
+    x += from_lane<0x118, 0xf>(x);
+    x += from_lane<0x142, 0xa>(x);      // the last lane of rows 0 and 2 into rows 1 and 3
+    x += from_lane<0x143, 0xc>(x);      // lane 31 into rows 2 and 3
+    return x;
+}
 
 // log2 of a page size, or -1 where it is none: a power of two from 16 (the attention reads sixteen rows of a page at a time) to 2^20.
 inline int page_shift(int page_size) {

@@ -79,16 +79,15 @@ def test_prepare_refusals():
     rows = (ctypes.c_int64 * 24)(*[x for i in range(6) for x in (0x1000000 * (i + 1), 4096, 512, 128)])
     where = ctypes.addressof(rows)
     cache = cache_struct()
-    base = dict(q=where, k=where + 32, v=where + 64, q_out=where + 96, k_out=where + 128, v_out=where + 160,
-                cache=ctypes.addressof(cache), slots=0x9000000, positions=0x9100000, qw=0x9200000, kw=0x9300000, eps=1e-6,
+    base = dict(rows=where, cache=ctypes.addressof(cache), slots=0x9000000, positions=0x9100000, qw=0x9200000, kw=0x9300000, eps=1e-6,
                 f=0x9400000, rotated=128, inter=0, B=2, N=8, H=4, KH=2, d=128, dtype=0)
 
     def call(**kw):
         return L.attn_qkv_prepare(*dict(base, **kw).values(), None)
     bad, no = binding.ERR_INVALID_ARG, binding.ERR_UNSUPPORTED
-    for name in ("q", "k", "v", "q_out", "positions", "f"):
+    for name in ("rows", "positions", "f"):
         refused(call(**{name: None}), bad, "non-null")
-    for name in ("k_out", "v_out", "cache", "slots"):
+    for name in ("cache", "slots"):
         refused(call(**{name: None}), bad, "given together")
     for name in ("B", "N", "H", "KH", "d"):
         refused(call(**{name: 0}), bad, "positive")
@@ -104,7 +103,8 @@ def test_prepare_refusals():
         refused(call(**{name: base[name] + 8}), bad, "16-byte")
     refused(call(positions=0x9100002), bad, "aligned")
     refused(call(slots=0x9000004), bad, "aligned")
-    for i, value, text in ((0, 0, "16-byte"), (0, 0x1000008, "16-byte"), (9, 4097, "strides of rows"), (14, -512, "strides of rows"),
+    for i, value, text in ((0, 0, "non-null"), (4, 0, "non-null"), (8, 0, "non-null"), (12, 0, "non-null"), (16, 0, "given together"),
+                           (20, 0, "given together"), (0, 0x1000008, "16-byte"), (9, 4097, "strides of rows"), (14, -512, "strides of rows"),
                            (7, 4, "strides of rows"), (13, 0, "at least d"), (15, 64, "at least d"), (22, 64, "at least d")):
         kept, rows[i] = rows[i], value
         refused(call(), bad, text)
