@@ -33,7 +33,6 @@ constexpr int kDecodeWaves = 4;                                  // of a workgro
 constexpr int kDecodeTile = 32;                                  // keys a wavefront takes at a time
 constexpr int kDecodeStep = kDecodeTile * kDecodeWaves;          // keys such a workgroup takes at a time: what is dealt out
 constexpr int kDecodeHeads = 16;                                 // query heads of a unit
-constexpr int kDecodeDirectWaves = 8;                            // of a workgroup that takes whole units
 constexpr long long kDecodeDirectFew = 1 << 18, kDecodeDirectMany = 1 << 20;      // bytes of K and V of a unit at most, with fewer or more units than compute units
 constexpr int kDecodeGrid = 1024;                                // workgroups that share units: at most
 constexpr int kDecodeUnits = 256;                                // compute units: up to as many workgroups of one step, then of two at least
@@ -185,40 +184,48 @@ struct DecodeState {
         l = 0.f;
     }
 
+    // BRIEF: of a tile at an edge only the rows are read that are visible, in loads of four or eight (where requests are short, edges are most of
+    // what there is; else the branches cost more than the rows: 64 ragged requests up to 8192, 94 and 97 us).
+    template <bool BRIEF>
     __device__ __forceinline__ void add(const DecodeParams& p, const DecodeLane<D>& lane, const DecodeUnit& u, const u4 (&q)[D / 32], const DecodePages& pages, int tile,
                                         LDS_PTR(char) lds) {
         using L = DecodeLane<D>;
         const int mask = (1 << p.shift) - 1, key0 = tile * kDecodeTile;
+        const bool edge = key0 < u.low || key0 + kDecodeTile > u.length;
         bool bad[2];
         unsigned v[8][D / 32];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            bad[half] = (unsigned)pages.half[half] >= (unsigned)p.pages;
-            const int page = bad[half] ? 0 : pages.half[half], row = (key0 + half * 16) & mask;
-            const char* k = u.K + page * p.k_page + (long long)row * p.k_row;
+        for (int half = 0; half < 2; ++half) bad[half] = (unsigned)pages.half[half] >= (unsigned)p.pages;
+        auto load = [&](auto all) {
+            constexpr bool ALL = decltype(all)::value;
+            auto wanted = [&](int first, int rows) { return ALL || (key0 + first < u.length && key0 + first + rows > u.low); };
 #pragma unroll
-            for (int i = 0; i < L::kLoads / 2; ++i)
-                load_to_lds_16B_nt(k + (long long)i * L::kRowsPerLoad * p.k_row, lane.k_from(i),
-                                   (unsigned)(uintptr_t)lds + (half * (L::kLoads / 2) + i) * 1024);
-        }
+            for (int half = 0; half < 2; ++half) {
+                const int page = bad[half] ? 0 : pages.half[half], row = (key0 + half * 16) & mask;
+                const char* k = u.K + page * p.k_page + (long long)row * p.k_row;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int page = bad[half] ? 0 : pages.half[half], row = (key0 + half * 16) & mask;
-            const char* from = u.V + page * p.v_page + (long long)row * p.v_row;
+                for (int i = 0; i < L::kLoads / 2; ++i)
+                    if (wanted(half * 16 + i * L::kRowsPerLoad, L::kRowsPerLoad))
+                        load_to_lds_16B_nt(k + (long long)i * L::kRowsPerLoad * p.k_row, lane.k_from(i),
+                                           (unsigned)(uintptr_t)lds + (half * (L::kLoads / 2) + i) * 1024);
+            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const char* at = from + (long long)i * 4 * p.v_row;
-                if constexpr (D == 128) {
-                    const u4 w = __builtin_nontemporal_load(reinterpret_cast<const u4*>(at + lane.v_from));
+            for (int half = 0; half < 2; ++half) {
+                const int page = bad[half] ? 0 : pages.half[half], row = (key0 + half * 16) & mask;
+                const char* from = u.V + page * p.v_page + (long long)row * p.v_row;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) v[half * 4 + i][x] = w[x];
-                } else {
-                    const u2 w = __builtin_nontemporal_load(reinterpret_cast<const u2*>(at + lane.v_from));
+                for (int i = 0; i < 4; ++i) {
+                    const char* at = from + (long long)i * 4 * p.v_row + lane.v_from;
+                    typedef unsigned words __attribute__((ext_vector_type(D / 32)));
+                    words w = {};
+                    if (wanted(half * 16 + i * 4, 4)) w = __builtin_nontemporal_load(reinterpret_cast<const words*>(at));
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) v[half * 4 + i][x] = w[x];
+                    for (int x = 0; x < D / 32; ++x) v[half * 4 + i][x] = w[x];
                 }
             }
-        }
+        };
+        if (BRIEF && edge) load(std::false_type{});
+        else load(std::true_type{});
         wait_tile_landed();
         f4 s[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
@@ -228,7 +235,7 @@ struct DecodeState {
                 s[half] = decode_mfma<BF16>(*(LDS_PTR(const u4))(lds + lane.k_operand(x) + half * 16 * L::kRowBytes), q[x], s[half]);
 #pragma unroll
         for (int half = 0; half < 2; ++half) s[half] *= p.c;
-        if (key0 < u.low || key0 + kDecodeTile > u.length || bad[0] || bad[1]) {
+        if (edge || bad[0] || bad[1]) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int key = key0 + 4 * i + lane.g;
@@ -327,7 +334,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void decode_kernel(DecodeParams p) {
             do {
                 const int next = tile + WAVES;
                 const DecodePages ahead(p, u, next);      // (behind the last one the last page again)
-                state.add(p, lane, u, q, pages, tile, (LDS_PTR(char))area[wave]);
+                state.template add<DIRECT && WAVES < 8>(p, lane, u, q, pages, tile, (LDS_PTR(char))area[wave]);
                 pages = ahead;
                 tile = next;
             } while (tile < tiles);
@@ -461,6 +468,7 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(DecodeParams 
 // The launch for a problem, from what the host knows.
 struct DecodePlan {
     int group, head_groups, units, heads_kept, grid;
+    int seen;         // rows of a unit, with every table full
     bool direct;
 };
 
@@ -474,14 +482,14 @@ int decode_plan(const sawattn_kv_cache* cache, int R, int H, int max_pages, int 
     out->head_groups = (out->group + kDecodeHeads - 1) / kDecodeHeads;
     out->units = out->head_groups * cache->heads;
     out->heads_kept = std::min(out->group, kDecodeHeads);
-    const long long seen = window > 0 ? std::min<long long>(capacity, window) : capacity;      // rows of a unit, with every table full
+    out->seen = (int)(window > 0 ? std::min<long long>(capacity, window) : capacity);
     const double most = (double)R * out->units * ((capacity + kDecodeStep - 1) / kDecodeStep);      // steps
     if (most >= 2147483648.0 - 2.0 * kDecodeGrid)
         return fail(SAWATTN_ERR_INVALID_ARG, "R*H*ceil(max_pages*page_size/128) must be below 2^31 - 2048");
     // One workgroup reads about 55 GB/s, the second kernel costs 6 us and more.  Few units: up to 500 keys at d = 128 take 8.5 us in one launch,
     // in two 9; 1000 keys 12.5 and 9.4.  Units for every compute unit and more: 256 requests of 1000 keys, 8 heads: 170 and 190 us, 128 ragged
     // requests up to 2000: 57 and 62.
-    const long long units = (long long)R * out->units, bytes = seen * 4 * cache->d;
+    const long long units = (long long)R * out->units, bytes = 4LL * out->seen * cache->d;
     out->direct = bytes <= (units >= kDecodeUnits ? kDecodeDirectMany : kDecodeDirectFew);
     out->grid = out->direct ? (int)units : (int)std::min<double>(most, cache->d == 128 ? kDecodeGrid / 2 : kDecodeGrid);
     return SAWATTN_OK;
@@ -490,7 +498,14 @@ int decode_plan(const sawattn_kv_cache* cache, int R, int H, int max_pages, int 
 template <int D, bool BF16>
 int launch_decode(const DecodeParams& p, const DecodePlan& plan, int H, hipStream_t stream) {
     if (plan.direct) {
-        hipLaunchKernelGGL((decode_kernel<D, BF16, kDecodeDirectWaves, true>), dim3(plan.grid), dim3(64 * kDecodeDirectWaves), 0, stream, p);
+        // A wavefront to a tile, up to eight of them; half as many where there are four units and more for every compute unit.  Measured with one
+        // wavefront, with two and with eight, two tiles at most: 149 requests of 4 rows, 16 key/value heads 7.8, 9.5, 21.2 us; one of 60 rows, 8 heads
+        // 6.0, 4.5, 4.7; 256 of 60 rows 14.2, 14.1, 20.5.  With two, four and eight, four tiles: 8 of 120 rows 6.3, 5.3, 5.5; 256 of 120 rows 24.2, 23.9, 29.7.
+        const int tiles = (plan.seen + kDecodeTile - 1) / kDecodeTile, wanted = plan.grid >= 4 * kDecodeUnits ? (tiles + 1) / 2 : tiles;
+        if (wanted <= 1) hipLaunchKernelGGL((decode_kernel<D, BF16, 1, true>), dim3(plan.grid), dim3(64), 0, stream, p);
+        else if (wanted <= 2) hipLaunchKernelGGL((decode_kernel<D, BF16, 2, true>), dim3(plan.grid), dim3(128), 0, stream, p);
+        else if (wanted <= 4) hipLaunchKernelGGL((decode_kernel<D, BF16, 4, true>), dim3(plan.grid), dim3(256), 0, stream, p);
+        else hipLaunchKernelGGL((decode_kernel<D, BF16, 8, true>), dim3(plan.grid), dim3(512), 0, stream, p);
         return launched("attn_decode");
     }
     hipLaunchKernelGGL((decode_kernel<D, BF16, kDecodeWaves, false>), dim3(plan.grid), dim3(64 * kDecodeWaves), 0, stream, p);

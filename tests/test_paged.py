@@ -486,6 +486,73 @@ def test_decode_lengths(lengths, KH, G, d):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("most", [1, 16, 32, 47, 64, 100, 128, 200, 256, 300, 512])
+@pytest.mark.parametrize("R,KH,G", [(5, 2, 3), (150, 8, 1)])
+def test_decode_short_tables(most, R, KH, G):
+    """Tables of few rows: one, two, four and eight wavefronts to a unit, with few units and with more than a thousand; what lies behind
+    the lengths, and in front of a window, is NaN."""
+    lengths = [(7 * i) % (most + 1) for i in range(R)]
+    lengths[0] = most
+    for d, dtype in ((64, "f16"), (128, "bf16")):
+        cache, table, keys = fill_cache(lengths, KH, d, 16, dtype, seed=most)
+        q, lens = queries(R, KH * G, d, dtype, seed=2), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+        assert binding.attn_decode_workspace_bytes(R, KH * G, cache, table.shape[1]) == 0
+        check_decode(binding.attn_decode(q, cache, table, lens, scale=d ** -0.5), q, keys, d ** -0.5, lengths)
+        window = most // 2 + 1
+        check_decode(binding.attn_decode(q, cache, table, lens, scale=d ** -0.5, window=window), q, keys, d ** -0.5, lengths, window)
+
+
+@pytest.mark.gpu
+def test_binding_refusals():
+    """What the calls refuse before they reach the library: types, shapes, sizes."""
+    cache, table, _ = fill_cache([20, 40], 2, 64, 16, "f16", seed=1)
+    q, lens = queries(2, 4, 64, "f16", seed=1), torch.tensor([20, 40], dtype=torch.int32, device="cuda")
+    pos = torch.zeros(2, dtype=torch.int32, device="cuda")
+    ok = dict(scale=0.1)
+    for args, kw in (((q.float(), cache, table, lens), ok), ((q[0], cache, table, lens), ok), ((q[:, :, :32], cache, table, lens), ok),
+                     ((q.cpu(), cache, table, lens), ok), ((q, cache, table.long(), lens), ok), ((q, cache, table[:1], lens), ok),
+                     ((q, cache, table.t().contiguous().t(), lens), ok), ((q, cache, table, lens.long()), ok), ((q, cache, table, lens[:1]), ok),
+                     ((q, cache, table, lens.cpu()), ok), ((q, cache, table, lens, q.double()), ok), ((q, cache, table, lens, q[:1]), ok),
+                     ((q, cache, table, lens), dict(scale=0.1, workspace=torch.zeros(9)))):
+        with pytest.raises(ValueError):
+            binding.attn_decode(*args, **kw)
+    with pytest.raises(binding.SawattnError, match="multiple"):
+        binding.attn_decode(q[:, :3], cache, table, lens, scale=0.1)
+    with pytest.raises(binding.SawattnError, match="scale"):
+        binding.attn_decode(q, cache, table, lens, scale=math.nan)
+    with pytest.raises(binding.SawattnError, match="smaller"):
+        long = torch.zeros(2, 600, dtype=torch.int32, device="cuda")
+        binding.attn_decode(q, cache, long, lens, scale=0.1, workspace=torch.zeros(64, device="cuda"))
+    for k, v in ((cache.k, cache.v[:, :1]), (cache.k.float(), cache.v.float()), (cache.k, cache.v.bfloat16()), (cache.k[0], cache.v[0]),
+                 (cache.k.transpose(2, 3), cache.v.transpose(2, 3)), (cache.k, cache.v.cpu())):
+        with pytest.raises(ValueError):
+            binding.KVCache(k, v)
+    k, slots, f, w = q[:, :2], torch.zeros(2, dtype=torch.int64, device="cuda"), frequencies(64), torch.ones(64, device="cuda")
+    good = dict(positions=pos, frequencies=f, cache=cache, slots=slots, q_weight=w)
+    binding.attn_qkv_prepare(q, k, k, **{**good, "slots": slots - 1})
+    for change in (dict(positions=pos.long()), dict(positions=pos[:1]), dict(slots=None), dict(slots=pos), dict(q_weight=w.half()), dict(q_weight=w[:8]),
+                   dict(frequencies=f.float()), dict(k_out=k), dict(k_out=k, v_out=k.float()), dict(q_out=q[:, :2]), dict(positions=pos.cpu())):
+        with pytest.raises(ValueError):
+            binding.attn_qkv_prepare(q, k, k, **{**good, **change})
+    for args in ((q, k.float(), k), (q, k, k[:1]), (q, k[:, :, :32], k), (q.float(), k, k), (q, k.cpu(), k), (q[0], k, k)):
+        with pytest.raises(ValueError):
+            binding.attn_qkv_prepare(*args, **good)
+    with pytest.raises(binding.SawattnError, match="rotated"):
+        binding.attn_qkv_prepare(q, k, k, **{**good, "frequencies": f[:3]})
+    ring, state = torch.arange(8, dtype=torch.int32, device="cuda"), torch.tensor([0, 8], dtype=torch.int32, device="cuda")
+    call = lambda **kw: binding.attn_kv_pages(*[kw.pop(n, x) for n, x in (("lengths", lens), ("new", pos), ("table", table), ("ring", ring), ("state", state))],
+                                              **{"page_size": 16, "tokens": 4, **kw})
+    call()
+    for change in (dict(lengths=lens.long()), dict(new=pos[:1]), dict(table=table.long()), dict(ring=ring.float()), dict(state=ring), dict(tokens=None),
+                   dict(slots=slots), dict(slots=pos, tokens=2), dict(positions=pos), dict(granted=pos[:1]), dict(free_state_out=ring), dict(new=pos.cpu()),
+                   dict(token_offsets=pos), dict(lengths=lens.cpu())):
+        with pytest.raises(ValueError):
+            call(**change)
+    with pytest.raises(binding.SawattnError, match="overlap"):
+        call(lengths_out=lens)
+
+
+@pytest.mark.gpu
 def test_decode_peaks_and_tiny_weights():
     """One row that outweighs a hundred thousand others, first, last and in the middle; and others that together outweigh it."""
     n, d = 100000, 64
