@@ -2,8 +2,8 @@
 //
 //   s_j = scale q . k_j,  o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m)   over the visible rows j of a request
 //
-// Bound by memory: every key and value is read once, for 4 d flops per query head that shares it.  A unit is a request, a key/value
-// head and up to 16 of its query heads.
+// Bound by memory: every key and value is read once, for 4 d flops per query head that shares it.  A unit is a request and a key/value
+// head, with up to 16 of its query heads; for more there is a set of workgroups for every 16 (a head group).
 //
 // Who does what.  Where a unit is short (below) a workgroup of eight wavefronts takes all of it: one launch.  Else the units' rows are cut into steps
 // of 128, and the steps of all units, one behind the other, are dealt out evenly: workgroup w takes `share` of them from w * share on, whatever the
@@ -54,10 +54,17 @@ struct DecodeParams {
     float c;             // scale * log2(e)
     int o_dtype, R, capacity, window, pages, shift;
     int group;           // query heads per key/value head
-    int head_groups;     // units per request and key/value head
-    int units;           // per request
+    int head_groups;     // by which a key/value head's query heads go, 16 at a time
+    int units;           // per request: key/value heads
+    int workgroups;      // for each head group
     int heads_kept;      // of a unit: min(group, 16)
 };
+
+// Workgroups come in one set for each head group, which share their keys and values: the same workgroup of all sets on one XCD (blocks go
+// round the eight of them), one behind the other, so that what the first brings into the L2 the others find there.
+__device__ __forceinline__ int block_of(const DecodeParams& p, int workgroup, int head_group) {
+    return p.head_groups == 1 ? workgroup : (workgroup / 8 * p.head_groups + head_group) * 8 + workgroup % 8;
+}
 
 struct DecodeRequest {
     int length, low, first, steps;      // visible rows low .. length - 1, in steps from `first` on
@@ -81,9 +88,9 @@ struct DecodeShare {
         int all = DecodeRequest(p, given0).steps;
         for (int i = lane + 64; i < p.R; i += 64) all += DecodeRequest(p, p.lengths[i]).steps;
         const int total = __builtin_amdgcn_readlane(lanes_upto(all), 63) * p.units;
-        share = max((int)(((unsigned)total + grid - 1) / (unsigned)grid), total > kDecodeUnits ? 2 : 1);
-        const int at = wg * share;      // (below the total and twice the grid)
-        left = min(share, total - at);
+        share = max((int)(((unsigned)total + grid - 1) / (unsigned)grid), total > kDecodeUnits / p.head_groups ? 2 : 1);
+        const int at = min(wg, grid - 1) * share;      // (below the total and twice the grid)
+        left = wg < grid ? min(share, total - at) : 0;
         r = unit = t0 = length = 0;
         if (left <= 0) return;
         const int wanted = (unsigned)at / (unsigned)p.units;
@@ -295,14 +302,21 @@ __global__ __launch_bounds__(64 * WAVES, 4) void decode_kernel(DecodeParams p) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const DecodeLane<D> lane(p, tid & 63);
 
+    int workgroup = blockIdx.x, head_group = 0;
+    if (p.head_groups > 1) {
+        const int eight = blockIdx.x / 8;
+        head_group = eight % p.head_groups;
+        workgroup = eight / p.head_groups * 8 + blockIdx.x % 8;      // (up to seven behind the last)
+    }
     int r, unit, t0, left, share, length;
     if constexpr (DIRECT) {
-        r = blockIdx.x / p.units;
-        unit = blockIdx.x - r * p.units;
+        if (workgroup >= p.workgroups) return;
+        r = workgroup / p.units;
+        unit = workgroup - r * p.units;
         t0 = left = share = 0;
         length = __builtin_amdgcn_readfirstlane(p.lengths[r]);
     } else {
-        const DecodeShare mine(p, tid & 63, blockIdx.x, gridDim.x);
+        const DecodeShare mine(p, tid & 63, workgroup, p.workgroups);
         r = mine.r; unit = mine.unit; t0 = mine.t0; left = mine.left; share = mine.share; length = mine.length;
         if (left <= 0) {
             if (tid == 0) p.begun[blockIdx.x] = int4{-1, 0, 0, 0};
@@ -313,14 +327,13 @@ __global__ __launch_bounds__(64 * WAVES, 4) void decode_kernel(DecodeParams p) {
 
     do {
         const int t1 = min(request.steps, t0 + left);      // (not DIRECT)
-        const int kv_head = unit / p.head_groups, head0 = (unit - kv_head * p.head_groups) * kDecodeHeads;
-        const int heads = min(kDecodeHeads, p.group - head0);
-        const char* q_row = p.Q + r * p.q_request + (long long)(kv_head * p.group + head0) * p.q_head;
+        const int head0 = head_group * kDecodeHeads, heads = min(kDecodeHeads, p.group - head0);
+        const char* q_row = p.Q + r * p.q_request + (long long)(unit * p.group + head0) * p.q_head;
         u4 q[D / 32];
 #pragma unroll
         for (int x = 0; x < D / 32; ++x)
             q[x] = lane.c < heads ? *reinterpret_cast<const u4*>(q_row + lane.c * p.q_head + x * 64 + lane.g * 16) : u4{0, 0, 0, 0};
-        const DecodeUnit u = {p.K + kv_head * p.k_head, p.V + kv_head * p.v_head,
+        const DecodeUnit u = {p.K + unit * p.k_head, p.V + unit * p.v_head,
                               (const __attribute__((address_space(4))) int*)(uintptr_t)(p.table + r * p.table_stride), request.low, request.length};
         DecodeState<D, BF16> state;
         state.clear();
@@ -372,7 +385,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void decode_kernel(DecodeParams p) {
                 o += f * *reinterpret_cast<const f4*>(reinterpret_cast<const float*>(area[w]) + head * kPitch + at4);
             }
             if (whole) {
-                const long long row = r * p.o_request + (long long)(kv_head * p.group + head0 + head) * p.o_head;
+                const long long row = r * p.o_request + (long long)(unit * p.group + head0 + head) * p.o_head;
                 store_o(p.O + row + at4 * (p.o_dtype == SAWATTN_F32 ? 4 : 2), p.o_dtype, request.length ? o / l : o);
             } else {
                 *reinterpret_cast<f4*>(p.parts + ((long long)place * p.heads_kept + head) * D + at4) = o;
@@ -384,7 +397,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void decode_kernel(DecodeParams p) {
         if (left <= 0) {
             // what is missing of a unit begun here takes the workgroups behind this one, in whole shares
             if (tid == 0)
-                p.begun[blockIdx.x] = int4{t0 == 0 && !whole ? r : -1, unit, (int)blockIdx.x + (request.steps - t1 + share - 1) / max(share, 1), 0};
+                p.begun[blockIdx.x] = int4{t0 == 0 && !whole ? r : -1, unit, workgroup + (request.steps - t1 + share - 1) / max(share, 1), 0};
             return;
         }
         __syncthreads();
@@ -415,11 +428,15 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(DecodeParams 
                 for (int e = tid; e < H * kAcross; e += kJoinThreads)
                     store_o(p.O + r * p.o_request + e / kAcross * p.o_head + e % kAcross * 4 * o_size, p.o_dtype, f4{0.f, 0.f, 0.f, 0.f});
     if (unit.x < 0) return;
-    const int kv_head = unit.y / p.head_groups, head0 = (unit.y - kv_head * p.head_groups) * kDecodeHeads, head = blockIdx.y * kJoinHeads + of_head;
+    int first = blockIdx.x, head_group = 0;
+    if (p.head_groups > 1) {
+        head_group = blockIdx.x / 8 % p.head_groups;
+        first = blockIdx.x / 8 / p.head_groups * 8 + blockIdx.x % 8;
+    }
+    const int last = unit.z, head0 = head_group * kDecodeHeads, head = blockIdx.y * kJoinHeads + of_head;
     const bool mine = head < min(kDecodeHeads, p.group - head0);
     float m = -INFINITY, l = 0.f;
     f4 o = {0.f, 0.f, 0.f, 0.f};
-    const int first = blockIdx.x, last = unit.z;
     if (mine) {
         for (int w = first + group; w <= last; w += kGroups * kJoinAhead) {
             f2 sums[kJoinAhead];
@@ -428,7 +445,7 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(DecodeParams 
 #pragma unroll
             for (int i = 0; i < kJoinAhead; ++i) {
                 const int at = min(w + i * kGroups, last);
-                const long long place = (long long)(2 * at + (at == first ? 1 : 0)) * p.heads_kept + head;
+                const long long place = (long long)(2 * block_of(p, at, head_group) + (at == first ? 1 : 0)) * p.heads_kept + head;
                 sums[i] = p.part_sums[place];
                 part[i] = *reinterpret_cast<const f4*>(p.parts + place * D + a * 4);
             }
@@ -462,12 +479,12 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(DecodeParams 
         l += f * sums_of[i][of_head][1];
         o += f * o_of[i][of_head][a];
     }
-    store_o(p.O + unit.x * p.o_request + (long long)(kv_head * p.group + head0 + head) * p.o_head + a * 4 * o_size, p.o_dtype, o / l);
+    store_o(p.O + unit.x * p.o_request + (long long)(unit.y * p.group + head0 + head) * p.o_head + a * 4 * o_size, p.o_dtype, o / l);
 }
 
 // The launch for a problem, from what the host knows.
 struct DecodePlan {
-    int group, head_groups, units, heads_kept, grid;
+    int group, head_groups, units, heads_kept, workgroups, grid;
     int seen;         // rows of a unit, with every table full
     bool direct;
 };
@@ -480,7 +497,7 @@ int decode_plan(const sawattn_kv_cache* cache, int R, int H, int max_pages, int 
     if (capacity > (1LL << 30)) return fail(SAWATTN_ERR_INVALID_ARG, "max_pages*page_size must be at most 2^30");
     out->group = H / cache->heads;
     out->head_groups = (out->group + kDecodeHeads - 1) / kDecodeHeads;
-    out->units = out->head_groups * cache->heads;
+    out->units = cache->heads;
     out->heads_kept = std::min(out->group, kDecodeHeads);
     out->seen = (int)(window > 0 ? std::min<long long>(capacity, window) : capacity);
     const double most = (double)R * out->units * ((capacity + kDecodeStep - 1) / kDecodeStep);      // steps
@@ -489,9 +506,13 @@ int decode_plan(const sawattn_kv_cache* cache, int R, int H, int max_pages, int 
     // One workgroup reads about 55 GB/s, the second kernel costs 6 us and more.  Few units: up to 500 keys at d = 128 take 8.5 us in one launch,
     // in two 9; 1000 keys 12.5 and 9.4.  Units for every compute unit and more: 256 requests of 1000 keys, 8 heads: 170 and 190 us, 128 ragged
     // requests up to 2000: 57 and 62.
-    const long long units = (long long)R * out->units, bytes = 4LL * out->seen * cache->d;
-    out->direct = bytes <= (units >= kDecodeUnits ? kDecodeDirectMany : kDecodeDirectFew);
-    out->grid = out->direct ? (int)units : (int)std::min<double>(most, cache->d == 128 ? kDecodeGrid / 2 : kDecodeGrid);
+    const long long units = (long long)R * out->units, bytes = 4LL * out->seen * cache->d, sets = out->head_groups;
+    out->direct = bytes <= (units * sets >= kDecodeUnits ? kDecodeDirectMany : kDecodeDirectFew);
+    const long long resident = (cache->d == 128 ? kDecodeGrid / 2 : kDecodeGrid) / sets, workgroups = out->direct ? units : std::min<long long>((long long)most, std::max(8LL, resident));
+    const long long grid = sets == 1 ? workgroups : (workgroups + 7) / 8 * 8 * sets;
+    if (grid >= (1LL << 31)) return fail(SAWATTN_ERR_INVALID_ARG, "R*H is too large");
+    out->workgroups = (int)workgroups;
+    out->grid = (int)grid;
     return SAWATTN_OK;
 }
 
@@ -589,7 +610,7 @@ int attn_decode(const void* Q, int64_t q_request, int64_t q_head, void* O, int64
     }
     p.c = (float)((double)scale * 1.4426950408889634074);
     p.R = R; p.capacity = max_pages * cache->page_size; p.window = window; p.pages = cache->pages; p.shift = page_shift(cache->page_size);
-    p.group = plan.group; p.head_groups = plan.head_groups; p.units = plan.units; p.heads_kept = plan.heads_kept;
+    p.group = plan.group; p.head_groups = plan.head_groups; p.units = plan.units; p.workgroups = plan.workgroups; p.heads_kept = plan.heads_kept;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const bool bf = cache->dtype == SAWATTN_BF16;
     if (d == 128) return bf ? launch_decode<128, true>(p, plan, H, stream) : launch_decode<128, false>(p, plan, H, stream);

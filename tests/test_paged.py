@@ -474,7 +474,8 @@ def test_decode_window(window, d, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("lengths,KH,G,d", [([200001], 1, 2, 128), ([70000, 3, 0, 33], 2, 1, 64), ([1] * 700, 4, 2, 128), ([97] * 300, 8, 1, 64),
-                                            (list(range(0, 2100, 7)), 1, 4, 64), ([40000] + [2] * 200, 2, 3, 128)])
+                                            (list(range(0, 2100, 7)), 1, 4, 64), ([40000] + [2] * 200, 2, 3, 128),
+                                            ([3000, 9001, 0, 77], 2, 35, 64)])
 def test_decode_lengths(lengths, KH, G, d):
     """One long request, many short ones, both: units spread over many workgroups, and many units to a workgroup."""
     cache, table, keys = fill_cache(lengths, KH, d, 64, "bf16", seed=9)
@@ -487,7 +488,7 @@ def test_decode_lengths(lengths, KH, G, d):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("most", [1, 16, 32, 47, 64, 100, 128, 200, 256, 300, 512])
-@pytest.mark.parametrize("R,KH,G", [(5, 2, 3), (150, 8, 1)])
+@pytest.mark.parametrize("R,KH,G", [(5, 2, 3), (150, 8, 1), (9, 1, 33)])
 def test_decode_short_tables(most, R, KH, G):
     """Tables of few rows: one, two, four and eight wavefronts to a unit, with few units and with more than a thousand; what lies behind
     the lengths, and in front of a window, is NaN."""
