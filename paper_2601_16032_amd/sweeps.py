@@ -1,4 +1,4 @@
-"""The paper's cache studies as sweeps over the attention kernel (one GPU).
+"""The paper's cache studies as sweeps over the attention kernel, and decoding steps over a paged cache (one GPU).
 
 Each study is a list of points (shape, launch variant, scan order).  A point is run as
 `--warmup` untimed plus `--launches` timed launches of the HIP kernel through the C ABI (after `--settle-ms`
@@ -20,6 +20,9 @@ Studies
   batch     Sec. 4.2 / 4.3 shapes: d = 64, N = 128K (and 32K), B in {1, 2, 4, 8}, plain and causal.
   heads     Alg. 2 against Alg. 3 where heads are short and come several to an XCD (B*H = 16...128, N = 512...8K):
             the persistent launch, the direct launch with one tile per workgroup, and what attn_fwd picks by itself.
+  steps     Decoding behind the prompt: one step (attn_kv_pages, attn_qkv_prepare, attn_decode) of R requests whose caches hold
+            `length` rows in pages of 64 in any order, ungrouped and grouped heads; each of the three timed for itself, with the bytes
+            per second that attn_decode reads of the cache.
 
 A point without a variant runs what attn_fwd runs (launch left open); a variant pins the persistent launch unless
 it names the other.  seqlen and batch are about rounds that share an L2 and pin the persistent launch, which attn_fwd
@@ -90,9 +93,77 @@ def study_points(study: str):
                     for var in ({"launch": "persistent", "kv_halves": 1},
                                 {"launch": "grid", "tiles_per_workgroup": 1, "kv_halves": 1}, {}):
                         pts.append(_pt(1, H, N, d, causal, "sawtooth", **var))
+    elif study == "steps":
+        for (H, KH, d) in ((8, 8, 64), (32, 32, 128), (32, 8, 128)):
+            for (R, length) in ((1, 255), (1, 16384), (1, 131071), (8, 4096), (64, 2048), (256, 512), (16, 32768)):
+                pts.append({"R": R, "length": length, "H": H, "KH": KH, "d": d})
     else:
         raise SystemExit(f"unknown study {study!r}")
     return pts
+
+
+STEP_PAGE_SIZE = 64
+
+
+def decode_step(pt, dtype="bf16", seed=0):
+    """One decoding step of a point of the study `steps` as a serving program holds it: [(operator, call)], to be called in order, and what they
+    work on.  The step can be repeated: lengths and the free list are written beside the ones it starts from."""
+    import torch
+    from . import binding as sa
+    R, length, H, KH, d = pt["R"], pt["length"], pt["H"], pt["KH"], pt["d"]
+    dt, ps = {"f16": torch.float16, "bf16": torch.bfloat16}[dtype], STEP_PAGE_SIZE
+    g = torch.Generator("cuda").manual_seed(seed)
+    held = -(-length // ps)
+    pages = R * (held + 1)                       # one more for each request's next token
+    order = torch.randperm(pages, generator=g, device="cuda").int()
+    table = torch.zeros(R, held + 1, dtype=torch.int32, device="cuda")
+    table[:, :held] = order[:R * held].view(R, held)
+    free = order.roll(-R * held)                 # the free ones first
+    state = torch.tensor([0, R], dtype=torch.int32, device="cuda")
+    cache = sa.KVCache(*(torch.randn(pages, KH, ps, d, generator=g, device="cuda", dtype=dt) for _ in range(2)))
+    qkv = torch.randn(R, H + 2 * KH, d, generator=g, device="cuda", dtype=dt)
+    weight = torch.ones(d, device="cuda")
+    frequencies = 1e4 ** (-torch.arange(0, d, 2, dtype=torch.float64, device="cuda") / d)
+    lengths = torch.full((R,), length, dtype=torch.int32, device="cuda")
+    new = torch.ones_like(lengths)
+    workspace = torch.empty(sa.attn_decode_workspace_bytes(R, H, cache, held + 1), dtype=torch.uint8, device="cuda")
+    step = sa.attn_kv_pages(lengths, new, table, free, state, page_size=ps, tokens=R)
+    held_by = {"qkv": qkv, "cache": cache, "table": table, "step": step, "weight": weight, "frequencies": frequencies,
+               "q": torch.empty(R, H, d, dtype=dt, device="cuda"), "o": torch.empty(R, H, d, dtype=dt, device="cuda")}
+    return [
+        ("attn_kv_pages", lambda: sa.attn_kv_pages(
+            lengths, new, table, free, state, page_size=ps, lengths_out=step.lengths, granted=step.granted,
+            token_offsets=step.token_offsets, free_state_out=step.free_state, slots=step.slots, positions=step.positions)),
+        ("attn_qkv_prepare", lambda: sa.attn_qkv_prepare(
+            qkv[:, :H], qkv[:, H:H + KH], qkv[:, H + KH:], positions=step.positions, frequencies=frequencies, q_weight=weight,
+            k_weight=weight, q_out=held_by["q"], cache=cache, slots=step.slots)),
+        ("attn_decode", lambda: sa.attn_decode(held_by["q"], cache, table, step.lengths, held_by["o"], scale=1.0 / math.sqrt(d),
+                                               workspace=workspace)),
+    ], held_by
+
+
+def run_steps(pts, chosen, args):
+    import torch
+    for i in chosen:
+        pt = pts[i]
+        calls, _ = decode_step(pt, seed=1234 + i)
+        out = {}
+        for name, call in calls:
+            for _ in range(args.warmup + 1):
+                call()
+            ev = [torch.cuda.Event(enable_timing=True) for _ in range(args.launches + 1)]
+            ev[0].record()
+            for k in range(args.launches):
+                for _ in range(8):               # back to back: the host's own time shows in the short ones all the same
+                    call()
+                ev[k + 1].record()
+            torch.cuda.synchronize()
+            out[name + "_us"] = round(sorted(ev[k].elapsed_time(ev[k + 1]) / 8e-3 for k in range(args.launches))[args.launches // 2], 2)
+        read = 4.0 * pt["R"] * (pt["length"] + 1) * pt["KH"] * pt["d"]
+        print(json.dumps({"study": "steps", "point": i, **pt, **out, "cache_gb_per_s": round(read / out["attn_decode_us"] / 1e3, 1)}), flush=True)
+        del calls
+        torch.cuda.empty_cache()
+    return 0
 
 
 def model(pt, info):
@@ -115,7 +186,7 @@ def model(pt, info):
 
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
-    ap.add_argument("--study", required=True, choices=["seqlen", "resident", "decode", "launch", "batch", "heads"])
+    ap.add_argument("--study", required=True, choices=["seqlen", "resident", "decode", "launch", "batch", "heads", "steps"])
     ap.add_argument("--points", default="", help="comma-separated point indices or a:b ranges (default: all)")
     ap.add_argument("--launches", type=int, default=3)
     ap.add_argument("--warmup", type=int, default=1)
@@ -145,6 +216,8 @@ def main(argv=None):
     if not torch.cuda.is_available():
         raise SystemExit("sweeps need a GPU (there is no CPU path)")
     sa.lib()
+    if args.study == "steps":
+        return run_steps(pts, chosen, args)
     stream = torch.cuda.current_stream()
     cache = {}
     dispatch = 0

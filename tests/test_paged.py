@@ -781,3 +781,32 @@ def test_decode_agrees_with_the_prompts_attention(dtype):
     # attn_fwd rounds probabilities to binary16: half a step of each
     size = (outs[2].float().abs().amax(2))
     assert ((whole[:, :, -1] - one).abs() <= 2.0 ** -11 * size + 2.0 ** -16 * size).all()
+
+
+def test_steps_study_lists_its_points(capsys):
+    from paper_2601_16032_amd import sweeps
+    assert sweeps.main(["--study", "steps", "--list"]) == 0
+    assert len(capsys.readouterr().out.splitlines()) == len(sweeps.study_points("steps")) == 21
+
+
+@pytest.mark.gpu
+def test_steps_study_runs(capsys):
+    """A point of the study `steps`: every operator timed, and the step right."""
+    import json
+    from paper_2601_16032_amd import sweeps
+    assert sweeps.main(["--study", "steps", "--points", "0,17", "--launches", "2"]) == 0
+    lines = [json.loads(x) for x in capsys.readouterr().out.splitlines() if x.startswith("{")]
+    assert [x["point"] for x in lines] == [0, 17] and all(x[n + "_us"] > 0 for x in lines for n in ("attn_kv_pages", "attn_qkv_prepare", "attn_decode"))
+    pt = {"R": 3, "length": 128, "H": 6, "KH": 3, "d": 64}
+    calls, held = sweeps.decode_step(pt, dtype="f16", seed=3)
+    for _ in range(2):
+        for _, call in calls:
+            call()
+    torch.cuda.synchronize()
+    cache, lengths = held["cache"], held["step"].lengths.tolist()
+    assert lengths == [129] * 3 and (held["table"].cpu().sort().values.diff() != 0).all()
+    keys = [[x[t.long()].transpose(1, 2).reshape(-1, 3, 64) for t in held["table"]] for x in (cache.k, cache.v)]
+    check_decode(held["o"], held["q"], keys, 0.125, lengths)
+    exact, size = po.rows(f64(held["qkv"][:, 6:9]), np.ones(64), 1e-6, np.full(3, 128), f64(held["frequencies"]), False)
+    check_rows(torch.stack([k[128] for k in keys[0]]), exact, size, torch.float16)
+    assert all(torch.equal(v[128], held["qkv"][r, 9:]) for r, v in enumerate(keys[1]))
