@@ -382,10 +382,10 @@ int attn_kv_pages(const int32_t* lengths, const int32_t* new_tokens, int R, int3
  *   frequencies        device, read: double [rotated / 2], radians per position, 16-byte aligned; NULL if rotated is 0
  *   rotated            0..d, a multiple of 8
  *   interleaved        0: element i is paired with i + rotated/2;  non-zero: 2i with 2i + 1
- *   B, N, H, KH        >= 1; B*N below 2^31, H + 2*KH at most 2^16
+ *   B, N, H, KH        >= 1; B*N below 2^26, H + 2*KH at most 2^16
  *   d, dtype           64 or 128, SAWATTN_F16 or SAWATTN_BF16, of all rows and of the cache
  * Other overlaps of outputs with inputs or with each other are not allowed (and not looked for).  Angles are reduced in 64 bits, all
- * else is computed in 32 and rounded once.  One launch; no workspace.  Stream and errors as attn_fwd.
+ * else is computed in 32 (squares of elements beyond 10^18 overflow) and rounded once.  One launch; no workspace.  Stream and errors as attn_fwd.
  */
 int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache* cache, const int64_t* slots, const int32_t* positions,
                      const float* q_weight, const float* k_weight, float eps, const double* frequencies, int rotated,
@@ -398,19 +398,21 @@ int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache* cache, con
  *
  *   Q                  device, read: [R][H][d], element e of head h at Q[r*q_request + h*q_head + e], 16-byte aligned, type of the cache
  *   O                  device, written, likewise with its own strides, element type o_dtype; every row of every request.  Must not
- *                      overlap Q, the cache or the workspace.
+ *                      overlap Q, the cache, the table, the lengths or the workspace (first to last byte, gaps included).
  *   strides            in elements, not negative, multiples of 8
  *   cache              host struct, read during the call; row strides at most 2^26
  *   table              device, read: int32 [R] rows of max_pages >= 1 entries, table_stride apart; max_pages*page_size at most 2^30,
  *                      R*H*ceil(max_pages*page_size/128) below 2^31 - 2048.
  *                      Entries behind the length's pages are not read as pages.
  *   lengths            device, read: int32 [R]; above max_pages*page_size they count as that, below 0 as 0
- *   R, H               >= 1, R*H below 2^31; H a multiple of cache->heads
+ *   R, H               >= 1, R*H below 2^22; H a multiple of cache->heads.  Up to 16 query heads share one reading of their keys and
+ *                      values, more read them once per 16.
  *   scale              finite
  *   window             >= 0; only rows lengths[r] - window and later are visible; 0: all
  *   workspace          device, written, 16-byte aligned, of at least attn_decode_workspace_bytes (NULL where that is 0); used by this call's kernels only, so
  *                      calls that overlap in time need one each.  Nothing in it has to start out zero.
- * A request of length 0 gets zeros.  A row of the cache behind the length is never used, whatever it holds.  A table entry outside
+ * A request of length 0 gets zeros.  A row of the cache outside the visible ones is never used, whatever it holds; an infinity among the visible
+ * values makes the elements it meets NaN.  A table entry outside
  * 0 .. pages - 1 among the visible ones makes the request's O NaN.  Products are exact, scores, probabilities, sums and O are held in 32 bits
  * (the probabilities enter the second product as sums of two 16-bit numbers).  The result does not depend on timing.
  * One launch where the rows that can be visible are few (up to 256 KiB of K and V per request and key/value head, or 1 MiB with

@@ -359,6 +359,14 @@ def _on(device, stream, call, *args):
         _check(rc)
 
 
+def _empty(shape, dtype, device, stream):
+    """A new tensor out of the memory of the stream that uses it first: memory of the current stream may still be in use there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _refuse_flat(device, *tensors):
     """Raise what is wrong with one of several (name, tensor, type, elements)."""
     for name, t, dtype, n in tensors:
@@ -394,13 +402,13 @@ def attn_kv_pages(lengths, new_tokens, table, free_pages, free_state, *, page_si
     if slots is None:
         if tokens is None:
             raise ValueError("either slots or the number of tokens must be given")
-        slots = torch.empty(tokens, dtype=i64, device=lengths.device)
+        slots = _empty(tokens, i64, lengths.device, stream)
     n, ring = slots.numel(), free_pages.numel()
     if tokens is not None and tokens != n:
         raise ValueError("slots must hold as many elements as there are tokens")
     if lengths_out is None or granted is None or token_offsets is None or free_state_out is None or positions is None:
         lengths_out, granted, token_offsets, free_state_out, positions = (
-            torch.empty(size, dtype=i32, device=lengths.device) if t is None else t for t, size in (
+            _empty(size, i32, lengths.device, stream) if t is None else t for t, size in (
                 (lengths_out, R), (granted, R), (token_offsets, R + 1), (free_state_out, 2), (positions, n)))
     if not (device >= 0 and lengths.dtype is i32 and lengths.is_contiguous()
             and new_tokens.dtype is i32 and new_tokens.numel() == R and new_tokens.get_device() == device and new_tokens.is_contiguous()
@@ -449,9 +457,9 @@ def attn_qkv_prepare(q, k, v, *, positions, frequencies=None, interleaved: bool 
     if (cache is None) != (slots is None) or (k_out is None) != (v_out is None):
         raise ValueError("cache and slots, and k_out and v_out, must be given together")
     if q_out is None:
-        q_out = torch.empty(shape, dtype=dtype, device=q.device)
+        q_out = _empty(shape, dtype, q.device, stream)
     if k_out is None and cache is None:
-        k_out, v_out = torch.empty(kv_shape, dtype=dtype, device=q.device), torch.empty(kv_shape, dtype=dtype, device=q.device)
+        k_out, v_out = _empty(kv_shape, dtype, q.device, stream), _empty(kv_shape, dtype, q.device, stream)
     if cache is not None and cache.device != device:
         raise ValueError("the cache must be on the other tensors' device")
     B, N, H, d = shape if len(shape) == 4 else (1, *shape)
@@ -502,13 +510,13 @@ def attn_decode(Q, cache: KVCache, table, lengths, O=None, *, scale: float, wind
         raise ValueError("Q must be a [R, H, d] tensor of the cache's device, dtype and d, contiguous in its last dimension")
     R, H, _ = shape
     if O is None:
-        O = torch.empty(shape, dtype=o_dtype or dtype, device=Q.device)
+        O = _empty(shape, o_dtype or dtype, Q.device, stream)
     o_stride, out = O.stride(), _DTYPE_CODE.get(O.dtype)
     if O.shape != shape or out is None or O.get_device() != device or o_stride[2] != 1:
         raise ValueError("O must be shaped like Q, on its device, contiguous in its last dimension (f16, bf16 or f32)")
     at, stride, wide = _page_table(table, R, device)
     if workspace is None:
-        workspace = torch.empty(attn_decode_workspace_bytes(R, H, cache, wide), dtype=torch.uint8, device=Q.device)
+        workspace = _empty(attn_decode_workspace_bytes(R, H, cache, wide), torch.uint8, Q.device, stream)
     if workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the other tensors' device")
     if lengths.dtype is not torch.int32 or lengths.numel() != R or lengths.get_device() != device or not lengths.is_contiguous():

@@ -491,7 +491,7 @@ struct DecodePlan {
 
 int decode_plan(const sawattn_kv_cache* cache, int R, int H, int max_pages, int window, DecodePlan* out) {
     if (R <= 0 || H <= 0 || max_pages <= 0) return fail(SAWATTN_ERR_INVALID_ARG, "R, H and max_pages must be positive");
-    if ((long long)R * H >= (1LL << 31)) return fail(SAWATTN_ERR_INVALID_ARG, "R*H must be below 2^31");
+    if ((long long)R * H >= (1LL << 22)) return fail(SAWATTN_ERR_INVALID_ARG, "R*H must be below 2^22");      // (a launch has fewer than 2^32 threads)
     if (H % cache->heads) return fail(SAWATTN_ERR_INVALID_ARG, "H must be a multiple of the cache's heads");
     const long long capacity = (long long)max_pages * cache->page_size;
     if (capacity > (1LL << 30)) return fail(SAWATTN_ERR_INVALID_ARG, "max_pages*page_size must be at most 2^30");
@@ -509,8 +509,7 @@ int decode_plan(const sawattn_kv_cache* cache, int R, int H, int max_pages, int 
     const long long units = (long long)R * out->units, bytes = 4LL * out->seen * cache->d, sets = out->head_groups;
     out->direct = bytes <= (units * sets >= kDecodeUnits ? kDecodeDirectMany : kDecodeDirectFew);
     const long long resident = (cache->d == 128 ? kDecodeGrid / 2 : kDecodeGrid) / sets, workgroups = out->direct ? units : std::min<long long>((long long)most, std::max(8LL, resident));
-    const long long grid = sets == 1 ? workgroups : (workgroups + 7) / 8 * 8 * sets;
-    if (grid >= (1LL << 31)) return fail(SAWATTN_ERR_INVALID_ARG, "R*H is too large");
+    const long long grid = sets == 1 ? workgroups : (workgroups + 7) / 8 * 8 * sets;      // (below 2^22 + 7 * 2^18)
     out->workgroups = (int)workgroups;
     out->grid = (int)grid;
     return SAWATTN_OK;

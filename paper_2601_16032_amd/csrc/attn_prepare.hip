@@ -192,8 +192,8 @@ extern "C" int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache*
     if (d != 64 && d != 128) return fail(SAWATTN_ERR_UNSUPPORTED, "head dimension must be 64 or 128");
     if (dtype != SAWATTN_F16 && dtype != SAWATTN_BF16)
         return fail(SAWATTN_ERR_INVALID_ARG, "dtype must be SAWATTN_F16 or SAWATTN_BF16");
-    if ((long long)B * N >= (1LL << 31) || H > (1 << 16) || KH > (1 << 16) || H + 2LL * KH > (1 << 16))
-        return fail(SAWATTN_ERR_INVALID_ARG, "B*N must be below 2^31 and H + 2*KH at most 2^16");
+    if ((long long)B * N >= (1LL << 26) || H > (1 << 16) || KH > (1 << 16) || H + 2LL * KH > (1 << 16))
+        return fail(SAWATTN_ERR_INVALID_ARG, "B*N must be below 2^26 and H + 2*KH at most 2^16");
     if (rotated < 0 || rotated > d || rotated % 8) return fail(SAWATTN_ERR_INVALID_ARG, "rotated must be a multiple of 8 from 0 to d");
     if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(SAWATTN_ERR_INVALID_ARG, "eps must be finite and not negative");
     if (!rows || !rows->q.data || !rows->k.data || !rows->v.data || !rows->q_out.data || !positions || (rotated && !frequencies))
@@ -244,8 +244,7 @@ extern "C" int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache*
     const int wanted = (int)std::min<long long>(all, (4096 + p.tokens - 1) / p.tokens);
     p.trips = (all + wanted - 1) / wanted;
     p.chunks = (all + p.trips - 1) / p.trips;
-    const long long waves = (long long)p.tokens * p.chunks;
-    if (waves >= (1LL << 31) - kPrepareThreads / 64) return fail(SAWATTN_ERR_INVALID_ARG, "too many tokens");
+    const long long waves = (long long)p.tokens * p.chunks;      // (below 2^26: 4096 tokens and more have one each, fewer at most 2^14)
     const int grid = (int)((waves + kPrepareThreads / 64 - 1) / (kPrepareThreads / 64));
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const bool bf = dtype == SAWATTN_BF16;

@@ -93,7 +93,7 @@ def test_prepare_refusals():
         refused(call(**{name: 0}), bad, "positive")
     refused(call(d=96), no, "head dimension")
     refused(call(dtype=2), bad, "dtype")
-    refused(call(B=2 ** 16, N=2 ** 15), bad, "B*N")
+    refused(call(B=2 ** 16, N=2 ** 10), bad, "B*N")
     refused(call(H=2 ** 16 - 1, KH=1), bad, "at most 2^16")
     for rotated in (-8, 4, 136):
         refused(call(rotated=rotated), bad, "rotated")
@@ -135,9 +135,9 @@ def test_decode_refusals():
     for name in ("R", "H", "wide"):
         refused(call(**{name: 0}), bad, "positive")
     refused(call(H=7), bad, "multiple of the cache's heads")
-    refused(call(R=2 ** 28, H=8), bad, "R*H")
+    refused(call(R=2 ** 20, H=8), bad, "R*H")
     refused(call(wide=2 ** 27, stride=2 ** 27), bad, "at most 2^30")
-    refused(call(R=2 ** 20, wide=2 ** 16, stride=2 ** 16), bad, "2^31 - 2048")
+    refused(call(R=2 ** 18, wide=2 ** 16, stride=2 ** 16), bad, "2^31 - 2048")
     refused(call(odt=3), bad, "o_dtype")
     for scale in (math.nan, math.inf):
         refused(call(scale=scale), bad, "scale")
@@ -589,10 +589,34 @@ def test_decode_whatever_the_tables_hold():
 
 
 @pytest.mark.gpu
+def test_decode_long_tables():
+    """Tables long enough for units in parts: nothing in them at all, a page outside the cache, lengths outside the table."""
+    for lengths in ([0] * 9, [0, 9000, 0]):
+        cache, table, keys = fill_cache(lengths, 2, 64, 16, "bf16", seed=3)
+        table = torch.cat([table, torch.full((len(lengths), 700 - table.shape[1]), POISON, dtype=torch.int32, device="cuda")], 1)
+        q, o = queries(len(lengths), 6, 64, "bf16", seed=1), torch.full((len(lengths), 6, 64), float("nan"), dtype=torch.bfloat16, device="cuda")
+        binding.attn_decode(q, cache, table, torch.tensor(lengths, dtype=torch.int32, device="cuda") - 4 * (torch.tensor(lengths, device="cuda") == 0).int(), o,
+                            scale=0.125)
+        check_decode(o, q, keys, 0.125, lengths)
+    real = [9008, 9008, 5, 9008]
+    cache, table, keys = fill_cache(real, 2, 64, 16, "f16", seed=4)
+    table[1, 77], table[3, 562] = 2 ** 31 - 1, cache.pages
+    given = torch.tensor([2 ** 31 - 1, 9008, 5, 9008], dtype=torch.int32, device="cuda")
+    q = queries(4, 6, 64, "f16", seed=1)
+    got = binding.attn_decode(q, cache, table, given, scale=0.125)
+    check_decode(got, q, keys, 0.125, real, skip=(1, 3))
+    assert got[1].isnan().all() and got[3].isnan().all()
+    got = binding.attn_decode(q, cache, table, given, scale=0.125, window=3000)
+    check_decode(got, q, keys, 0.125, real, 3000, skip=(3,))
+    assert got[3].isnan().all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
-def test_decode_keeps_what_is_no_number_to_itself(d):
-    """NaN and infinities among the visible rows reach the heads that see them and no others."""
-    lengths = [300, 300, 300]
+@pytest.mark.parametrize("length", [300, 6000])
+def test_decode_keeps_what_is_no_number_to_itself(d, length):
+    """NaN among the visible rows reaches the heads that see it and no others."""
+    lengths = [length] * 3
     cache, table, keys = fill_cache(lengths, 2, d, 16, "bf16", seed=8)
     cache.k[int(table[1, 3]), 0, 5, 11] = float("nan")      # request 1, key head 0
     cache.v[int(table[2, 18]), 1, 2, 7] = float("nan")      # request 2, key head 1, element 7
@@ -781,6 +805,30 @@ def test_decode_agrees_with_the_prompts_attention(dtype):
     # attn_fwd rounds probabilities to binary16: half a step of each
     size = (outs[2].float().abs().amax(2))
     assert ((whole[:, :, -1] - one).abs() <= 2.0 ** -11 * size + 2.0 ** -16 * size).all()
+
+
+def test_built_kernels(tmp_path):
+    """The kernels as built: none has scratch memory, and none reads K from LDS before the direct loads that bring it have landed."""
+    import re
+    from .util import device_code, device_listing, kernel_bodies, llvm_tool
+    notes = llvm_tool("llvm-readelf", "--notes", device_code(tmp_path))
+    found = dict(re.findall(r"\.name:\s+(_ZN7sawattn\d+(?:kv_pages|qkv_prepare|decode|decode_join)_kernel\S+)\s+\.private_segment_fixed_size:\s+(\d+)", notes, re.S))
+    assert len(found) >= 2 + 8 + 20 + 2 and set(found.values()) == {"0"}, found
+    (tmp_path / "listing").mkdir()
+    seen = 0
+    for kernel, body in kernel_bodies(device_listing(tmp_path / "listing")).items():
+        if "sawattn::decode_kernel<" not in kernel:
+            continue
+        flying, loads, waits = False, 0, 0
+        for text, _ in body:
+            if text.startswith("global_load_lds_"):
+                flying, loads = True, loads + 1
+            elif re.match(r"s_waitcnt .*vmcnt\(0\)", text):
+                flying, waits = False, waits + 1
+            assert not (flying and text.startswith("ds_")), (kernel, text)
+        assert loads >= 4 and waits and not flying, kernel
+        seen += 1
+    assert seen == 20
 
 
 def test_steps_study_lists_its_points(capsys):
