@@ -7,12 +7,11 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 from typing import NamedTuple
 
 import torch
 
-from .build import LIB_PATH, PROBE_LIB_PATH
+from .build import LIB_PATH, PAGED_BINDING_PATH, PROBE_LIB_PATH
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_RUNTIME = 0, 1, 2, 3
 SCAN_CYCLIC, SCAN_SAWTOOTH = 0, 1
@@ -336,14 +335,29 @@ class KVCache:
         self.ptr = ctypes.addressof(self._struct)
 
 
-# As with attn_fwd, a small call takes longer on the host than on the GPU: the calls below look at every tensor once, in one expression,
-# and find out what is wrong, if something is, in functions of their own.  Called in a row: attn_kv_pages 9.4 -> 7.8 us, attn_qkv_prepare
-# 10.9 -> 8.5, attn_decode in one launch 8.0 -> 6.7.
+_paged = None
+
+
+def _paged_module():
+    """The module that looks at tensors and calls the library for the three operators below (built with the library), bound to it."""
+    global _paged
+    if _paged is None:
+        if not os.path.exists(PAGED_BINDING_PATH):
+            raise FileNotFoundError(f"{PAGED_BINDING_PATH} is not built; run `python -m paper_2601_16032_amd.build` first")
+        L = lib()
+        from . import _paged as module
+        module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.attn_kv_pages, L.attn_qkv_prepare, L.attn_decode)))
+        _paged = module
+    return _paged
+
+
 _current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
 def _on(device, stream, call, *args):
     """call(*args, handle of the stream or of the device's current one) with `device` current; raises what the library refuses."""
+    if device < 0:
+        raise ValueError("the first tensor must be a device tensor")
     if stream is None:
         handle = _current_raw_stream(device)
     elif stream.device.index == device:
@@ -367,23 +381,6 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _refuse_flat(device, *tensors):
-    """Raise what is wrong with one of several (name, tensor, type, elements)."""
-    for name, t, dtype, n in tensors:
-        if t is not None and (t.dtype != dtype or t.numel() != n or t.get_device() != device or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on the other tensors' device")
-    raise ValueError("all tensors must be on one device, which must be a GPU")
-
-
-def _page_table(table, R, device):
-    """(address, stride, pages per request) of a page table"""
-    shape, stride = table.shape, table.stride()
-    if table.dtype is not torch.int32 or table.get_device() != device or len(shape) != 2 or shape[0] != R or stride[1] != 1 and shape[1] > 1:
-        raise ValueError("the page table must be an int32 [requests, pages] device tensor with contiguous rows")
-    wide = shape[1]
-    return table.data_ptr(), max(stride[0], wide) if R == 1 else stride[0], wide
-
-
 class PageStep(NamedTuple):
     """What attn_kv_pages writes."""
     lengths: torch.Tensor         # int32 [R]
@@ -398,50 +395,20 @@ def attn_kv_pages(lengths, new_tokens, table, free_pages, free_state, *, page_si
                   granted=None, token_offsets=None, free_state_out=None, slots=None, positions=None, stream=None) -> PageStep:
     """Pages, slots and positions of the tokens that `new_tokens` adds to requests of `lengths`; `table` and the ring `free_pages` are
     brought up to date in place, the rest is written to the tensors given or to new ones (`tokens` rows where no slots are given)."""
-    R, device, i32, i64 = lengths.numel(), lengths.get_device(), torch.int32, torch.int64
     if slots is None:
         if tokens is None:
             raise ValueError("either slots or the number of tokens must be given")
-        slots = _empty(tokens, i64, lengths.device, stream)
-    n, ring = slots.numel(), free_pages.numel()
-    if tokens is not None and tokens != n:
+        slots = _empty(tokens, torch.int64, lengths.device, stream)
+    elif tokens is not None and tokens != slots.numel():
         raise ValueError("slots must hold as many elements as there are tokens")
     if lengths_out is None or granted is None or token_offsets is None or free_state_out is None or positions is None:
+        R = lengths.numel()
         lengths_out, granted, token_offsets, free_state_out, positions = (
-            _empty(size, i32, lengths.device, stream) if t is None else t for t, size in (
-                (lengths_out, R), (granted, R), (token_offsets, R + 1), (free_state_out, 2), (positions, n)))
-    if not (device >= 0 and lengths.dtype is i32 and lengths.is_contiguous()
-            and new_tokens.dtype is i32 and new_tokens.numel() == R and new_tokens.get_device() == device and new_tokens.is_contiguous()
-            and free_pages.dtype is i32 and free_pages.get_device() == device and free_pages.is_contiguous()
-            and free_state.dtype is i32 and free_state.numel() == 2 and free_state.get_device() == device and free_state.is_contiguous()
-            and lengths_out.dtype is i32 and lengths_out.numel() == R and lengths_out.get_device() == device and lengths_out.is_contiguous()
-            and granted.dtype is i32 and granted.numel() == R and granted.get_device() == device and granted.is_contiguous()
-            and token_offsets.dtype is i32 and token_offsets.numel() == R + 1 and token_offsets.get_device() == device
-            and token_offsets.is_contiguous()
-            and free_state_out.dtype is i32 and free_state_out.numel() == 2 and free_state_out.get_device() == device
-            and free_state_out.is_contiguous()
-            and slots.dtype is i64 and slots.get_device() == device and slots.is_contiguous()
-            and positions.dtype is i32 and positions.numel() == n and positions.get_device() == device and positions.is_contiguous()):
-        _refuse_flat(device, ("lengths", lengths, i32, R), ("new_tokens", new_tokens, i32, R), ("free_pages", free_pages, i32, ring),
-                     ("free_state", free_state, i32, 2), ("lengths_out", lengths_out, i32, R), ("granted", granted, i32, R),
-                     ("token_offsets", token_offsets, i32, R + 1), ("free_state_out", free_state_out, i32, 2), ("slots", slots, i64, n),
-                     ("positions", positions, i32, n))
-    at, stride, wide = _page_table(table, R, device)
-    _on(device, stream, (_lib or lib()).attn_kv_pages, lengths.data_ptr(), new_tokens.data_ptr(), R, at, stride, wide, page_size,
-        free_pages.data_ptr(), ring, free_state.data_ptr(), lengths_out.data_ptr(), granted.data_ptr(), token_offsets.data_ptr(),
-        free_state_out.data_ptr(), slots.data_ptr(), positions.data_ptr(), n)
+            _empty(size, torch.int32, lengths.device, stream) if t is None else t for t, size in (
+                (lengths_out, R), (granted, R), (token_offsets, R + 1), (free_state_out, 2), (positions, slots.numel())))
+    _on(lengths.get_device(), stream, (_paged or _paged_module()).kv_pages, lengths, new_tokens, table, free_pages, free_state, lengths_out,
+        granted, token_offsets, free_state_out, slots, positions, page_size)
     return PageStep(lengths_out, granted, token_offsets, free_state_out, slots, positions)
-
-
-_pack_rows = struct.Struct("24q").pack       # sawattn_qkv: address and three strides of six tensors
-_NO_STRIDES = (0, 0, 0, 0)
-
-
-def _refuse_rows(dtype, device, *tensors):
-    """Raise what is wrong with one of several (name, tensor, shape)."""
-    for name, t, shape in tensors:
-        if t is not None and (t.shape != shape or t.dtype != dtype or t.get_device() != device or t.stride(-1) != 1):
-            raise ValueError(f"{name} must be a {list(shape)} {dtype} tensor on the other tensors' device, contiguous in its last dimension")
 
 
 def attn_qkv_prepare(q, k, v, *, positions, frequencies=None, interleaved: bool = False, q_weight=None, k_weight=None,
@@ -449,47 +416,18 @@ def attn_qkv_prepare(q, k, v, *, positions, frequencies=None, interleaved: bool 
     """Norms of the heads of Q and K (where a weight is given) and rotation of their first 2 * len(frequencies) elements, K and V
     written to `slots` of the cache and / or to k_out and v_out.  q, k, v: [B, N, heads, d] or [N, heads, d], of any strides.
     Returns (q_out, k_out, v_out); q_out is made where it is not given, k_out and v_out where there is no cache either."""
-    shape, kv_shape, dtype, device = q.shape, k.shape, q.dtype, q.get_device()
-    if len(shape) not in (3, 4) or dtype not in _IN_DTYPE_CODE or device < 0:
-        raise ValueError("q must be a [B, N, H, d] or [N, H, d] device tensor, float16 or bfloat16")
-    if kv_shape[:-2] != shape[:-2] or kv_shape[-1] != shape[-1] or len(kv_shape) != len(shape):
-        raise ValueError("q and k must share all dimensions but the heads")
     if (cache is None) != (slots is None) or (k_out is None) != (v_out is None):
         raise ValueError("cache and slots, and k_out and v_out, must be given together")
     if q_out is None:
-        q_out = _empty(shape, dtype, q.device, stream)
-    if k_out is None and cache is None:
-        k_out, v_out = _empty(kv_shape, dtype, q.device, stream), _empty(kv_shape, dtype, q.device, stream)
-    if cache is not None and cache.device != device:
-        raise ValueError("the cache must be on the other tensors' device")
-    B, N, H, d = shape if len(shape) == 4 else (1, *shape)
-    half = frequencies.numel() if frequencies is not None else 0
-    i32, i64, f32, f64 = torch.int32, torch.int64, torch.float32, torch.float64
-    if not (positions.dtype is i32 and positions.numel() == B * N and positions.get_device() == device and positions.is_contiguous()
-            and (slots is None or slots.dtype is i64 and slots.numel() == B * N and slots.get_device() == device and slots.is_contiguous())
-            and (q_weight is None or q_weight.dtype is f32 and q_weight.numel() == d and q_weight.get_device() == device
-                 and q_weight.is_contiguous())
-            and (k_weight is None or k_weight.dtype is f32 and k_weight.numel() == d and k_weight.get_device() == device
-                 and k_weight.is_contiguous())
-            and (frequencies is None or frequencies.dtype is f64 and frequencies.get_device() == device and frequencies.is_contiguous())):
-        _refuse_flat(device, ("positions", positions, i32, B * N), ("slots", slots, i64, B * N), ("q_weight", q_weight, f32, d),
-                     ("k_weight", k_weight, f32, d), ("frequencies", frequencies, f64, half))
-    qs, ks, vs, os_ = q.stride(), k.stride(), v.stride(), q_out.stride()
-    if not (v.shape == kv_shape and q_out.shape == shape and k.dtype is dtype and v.dtype is dtype and q_out.dtype is dtype
-            and k.get_device() == device and v.get_device() == device and q_out.get_device() == device
-            and qs[-1] == 1 and ks[-1] == 1 and vs[-1] == 1 and os_[-1] == 1):
-        _refuse_rows(dtype, device, ("q", q, shape), ("k", k, kv_shape), ("v", v, kv_shape), ("q_out", q_out, shape))
-    kos, vos, ko, vo = _NO_STRIDES, _NO_STRIDES, 0, 0
-    if k_out is not None:
-        _refuse_rows(dtype, device, ("k_out", k_out, kv_shape), ("v_out", v_out, kv_shape))
-        kos, vos, ko, vo = k_out.stride(), v_out.stride(), k_out.data_ptr(), v_out.data_ptr()
-    if len(shape) == 3:
-        qs, ks, vs, os_, kos, vos = ((0, *x) for x in (qs, ks, vs, os_, kos, vos))
-    rows = _pack_rows(q.data_ptr(), qs[0], qs[1], qs[2], k.data_ptr(), ks[0], ks[1], ks[2], v.data_ptr(), vs[0], vs[1], vs[2],
-                      q_out.data_ptr(), os_[0], os_[1], os_[2], ko, kos[0], kos[1], kos[2], vo, vos[0], vos[1], vos[2])
-    _on(device, stream, (_lib or lib()).attn_qkv_prepare, rows, None if cache is None else cache.ptr, None if slots is None else slots.data_ptr(),
-        positions.data_ptr(), None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), eps,
-        None if half == 0 else frequencies.data_ptr(), 2 * half, 1 if interleaved else 0, B, N, H, kv_shape[-2], d, _IN_DTYPE_CODE[dtype])
+        q_out = _empty(q.shape, q.dtype, q.device, stream)
+    if cache is None:
+        ptr, at = None, -1
+        if k_out is None:
+            k_out, v_out = _empty(k.shape, k.dtype, q.device, stream), _empty(k.shape, k.dtype, q.device, stream)
+    else:
+        ptr, at = cache.ptr, cache.device
+    _on(q.get_device(), stream, (_paged or _paged_module()).qkv_prepare, q, k, v, q_out, k_out, v_out, ptr, at, slots, positions, q_weight,
+        k_weight, eps, frequencies, interleaved)
     return q_out, k_out, v_out
 
 
@@ -505,22 +443,10 @@ def attn_decode(Q, cache: KVCache, table, lengths, O=None, *, scale: float, wind
     """O[r, h] = softmax(q . K^T * scale) V of one token per request, Q [R, H, d], over the last `window` (0: all) of the lengths[r]
     cached rows that table[r] names the pages of.  workspace: a uint8 tensor of at least attn_decode_workspace_bytes bytes, made
     here when None.  Returns O without waiting."""
-    shape, q_stride, device, dtype = Q.shape, Q.stride(), cache.device, Q.dtype
-    if len(shape) != 3 or Q.get_device() != device or dtype is not cache.dtype or q_stride[2] != 1 or shape[2] != cache.d:
-        raise ValueError("Q must be a [R, H, d] tensor of the cache's device, dtype and d, contiguous in its last dimension")
-    R, H, _ = shape
     if O is None:
-        O = _empty(shape, o_dtype or dtype, Q.device, stream)
-    o_stride, out = O.stride(), _DTYPE_CODE.get(O.dtype)
-    if O.shape != shape or out is None or O.get_device() != device or o_stride[2] != 1:
-        raise ValueError("O must be shaped like Q, on its device, contiguous in its last dimension (f16, bf16 or f32)")
-    at, stride, wide = _page_table(table, R, device)
+        O = _empty(Q.shape, o_dtype or Q.dtype, Q.device, stream)
     if workspace is None:
-        workspace = _empty(attn_decode_workspace_bytes(R, H, cache, wide), torch.uint8, Q.device, stream)
-    if workspace.get_device() != device or not workspace.is_contiguous():
-        raise ValueError("workspace must be a contiguous tensor on the other tensors' device")
-    if lengths.dtype is not torch.int32 or lengths.numel() != R or lengths.get_device() != device or not lengths.is_contiguous():
-        _refuse_flat(device, ("lengths", lengths, torch.int32, R))
-    _on(device, stream, (_lib or lib()).attn_decode, Q.data_ptr(), q_stride[0], q_stride[1], O.data_ptr(), o_stride[0], o_stride[1], out,
-        cache.ptr, at, stride, wide, lengths.data_ptr(), R, H, scale, window, workspace.data_ptr(), workspace.nbytes)
+        workspace = _empty(attn_decode_workspace_bytes(Q.shape[0], Q.shape[1], cache, table.shape[-1]), torch.uint8, Q.device, stream)
+    device = cache.device
+    _on(device, stream, (_paged or _paged_module()).decode, Q, O, cache.ptr, device, table, lengths, scale, window, workspace)
     return O

@@ -1,14 +1,16 @@
-"""Compile the HIP sources in csrc/ into libsawattn.so (in-tree, next to this file) for gfx950."""
+"""Compile the HIP sources in csrc/ into libsawattn.so (in-tree, next to this file) for gfx950, and the Python module beside it."""
 from __future__ import annotations
 
 import os
 import re
 import subprocess
+import sysconfig
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(_HERE), "include")
 LIB_PATH = os.path.join(_HERE, "libsawattn.so")
+PAGED_BINDING_PATH = os.path.join(_HERE, "_paged.so")         # Python module: tensors to addresses for the operators over a paged cache
 PROBE_LIB_PATH = os.path.join(_HERE, "libsawattn_probe.so")   # the benchmark's matrix-rate probe, not part of the path
 
 HIPCC_FLAGS = [
@@ -78,7 +80,24 @@ def build(verbose: bool = False) -> str:
                 raise
         if verbose:
             print(" ".join(cmd))
+    build_binding(verbose)
     return LIB_PATH
+
+
+def build_binding(verbose: bool = False) -> str:
+    """The Python module that hands tensors to the library: host code, against the headers of the interpreter and of torch."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", INCLUDE, "-I", sysconfig.get_paths()["include"], "-I", os.path.join(at, "include"),
+           "-I", os.path.join(at, "include", "torch", "csrc", "api", "include"), os.path.join(CSRC, "paged_binding.cpp"), "-o", PAGED_BINDING_PATH,
+           "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("the binding did not compile:\n" + res.stdout + res.stderr)
+    if verbose:
+        print(" ".join(cmd))
+    return PAGED_BINDING_PATH
 
 
 if __name__ == "__main__":
