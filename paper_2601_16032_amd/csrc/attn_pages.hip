@@ -10,6 +10,8 @@
 // every new page has exactly one token whose row is its first, and that token enters it into the table.
 namespace sawattn {
 
+constexpr int kPagesEach = 4;      // requests of a thread at most
+
 struct PagesParams {
     const int* lengths;
     const int* added;
@@ -36,9 +38,10 @@ struct PageRequest {
     int length, added;      // added < 0: ends
     int held, missing, back;
     bool fits;
-    __device__ __forceinline__ PageRequest(const PagesParams& p, int r) {
-        length = max(p.lengths[r], 0);
-        added = p.added[r];
+    __device__ __forceinline__ PageRequest() {}
+    __device__ __forceinline__ PageRequest(const PagesParams& p, int given, int new_tokens) {
+        length = max(given, 0);
+        added = new_tokens;
         const long long most = (long long)p.max_pages << p.shift, end = (long long)length + max(added, 0);
         const int round = (1 << p.shift) - 1;
         held = (int)(((long long)length + round) >> p.shift);
@@ -49,21 +52,35 @@ struct PageRequest {
     __device__ __forceinline__ PageSums sums() const { return {(long long)max(added, 0), missing, back}; }
 };
 
-// THREADS: 256, or 1024 for more than 1024 requests, so that four are left to a thread at most (4096 requests: 16.8 -> 10.3 us; but 257: 4.2 -> 4.6).
+// THREADS: 256, or 1024 for more than 1024 requests, which leaves a thread four at most (257 requests with 256 threads 4.2 us, with 1024 4.6).
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void kv_pages_kernel(PagesParams p) {
     __shared__ int tokens_upto[SAWATTN_MOST_REQUESTS];      // T_r
     __shared__ int back_upto[SAWATTN_MOST_REQUESTS];        // Q_r
     __shared__ int first_page[SAWATTN_MOST_REQUESTS];       // P_(r-1): its first new page, counted from the ring's first; -1: nothing granted
+    __shared__ int length_of[SAWATTN_MOST_REQUESTS];
     __shared__ PageSums of_wave[THREADS / 64];
     __shared__ int taken_by_wave[THREADS / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const unsigned F = (unsigned)p.ring_size;
     const int first_given = p.state[0], free_given = p.state[1];
-    const int each = (p.R + THREADS - 1) / THREADS, r0 = tid * each, r1 = min(p.R, r0 + each);
+    const int each = (p.R + THREADS - 1) / THREADS, r0 = tid * each;
 
+    // the thread's requests: all of their numbers on their way at once (and none read twice)
+    PageRequest request[kPagesEach];
+    int given[kPagesEach], added[kPagesEach];
+#pragma unroll
+    for (int i = 0; i < kPagesEach; ++i) {
+        const bool there = i < each && r0 + i < p.R;
+        given[i] = there ? p.lengths[r0 + i] : 0;
+        added[i] = there ? p.added[r0 + i] : 0;
+    }
     PageSums mine = {0, 0, 0};
-    for (int r = r0; r < r1; ++r) mine.add(PageRequest(p, r).sums());
+#pragma unroll
+    for (int i = 0; i < kPagesEach; ++i) {
+        request[i] = PageRequest(p, given[i], added[i]);
+        mine.add(request[i].sums());
+    }
     const PageSums upto = {lanes_upto(mine.tokens), lanes_upto(mine.missing), lanes_upto(mine.back)};
     if (lane == 63) of_wave[wave] = upto;
     __syncthreads();
@@ -78,8 +95,11 @@ __global__ __launch_bounds__(THREADS) void kv_pages_kernel(PagesParams p) {
     const unsigned first = first_given >= 0 && (unsigned)first_given < F ? (unsigned)first_given : 0u;
     const int available = min(max(free_given, 0), p.ring_size);
     int taken = 0;
-    for (int r = r0; r < r1; ++r) {
-        const PageRequest q(p, r);
+#pragma unroll
+    for (int i = 0; i < kPagesEach; ++i) {
+        const int r = r0 + i;
+        if (i >= each || r >= p.R) continue;
+        const PageRequest& q = request[i];
         PageSums with = before;
         with.add(q.sums());
         const bool there = with.missing <= available && with.tokens <= p.tokens;
@@ -89,6 +109,7 @@ __global__ __launch_bounds__(THREADS) void kv_pages_kernel(PagesParams p) {
         tokens_upto[r] = T;
         back_upto[r] = with.back;
         first_page[r] = ok ? before.missing : -1;
+        length_of[r] = q.length;
         if (blockIdx.x == 0) {
             p.lengths_out[r] = q.added < 0 ? 0 : ok ? q.length + q.added : q.length;
             p.granted[r] = ok ? q.added : 0;
@@ -121,7 +142,7 @@ __global__ __launch_bounds__(THREADS) void kv_pages_kernel(PagesParams p) {
                 if (tokens_upto[mid] > t) high = mid; else low = mid + 1;
             }
             if (first_page[low] >= 0) {
-                const int length = max(p.lengths[low], 0);
+                const int length = length_of[low];
                 row = length + t - (low ? tokens_upto[low - 1] : 0);
                 const int index = row >> p.shift, new_index = index - (int)(((long long)length + (1 << p.shift) - 1) >> p.shift);
                 int* entry = p.table + low * p.table_stride + index;
@@ -190,7 +211,8 @@ extern "C" int attn_kv_pages(const int32_t* lengths, const int32_t* new_tokens, 
                      free_state_out, reinterpret_cast<long long*>(slots), positions, R, max_pages, page_shift(page_size), ring, tokens};
     // 512 tokens to a workgroup, and a workgroup for every 64 requests at least, whose pages it may have to give back.
     const int grid = std::min(256, std::max((tokens + 511) / 512, (R + 63) / 64));
-    if (R <= 1024) hipLaunchKernelGGL((kv_pages_kernel<256>), dim3(grid), dim3(256), 0, static_cast<hipStream_t>(hip_stream), p);
+    static_assert(1024 * kPagesEach >= SAWATTN_MOST_REQUESTS, "a thread's requests");
+    if (R <= 256 * kPagesEach) hipLaunchKernelGGL((kv_pages_kernel<256>), dim3(grid), dim3(256), 0, static_cast<hipStream_t>(hip_stream), p);
     else hipLaunchKernelGGL((kv_pages_kernel<1024>), dim3(grid), dim3(1024), 0, static_cast<hipStream_t>(hip_stream), p);
     return launched("attn_kv_pages");
 }

@@ -4,10 +4,12 @@
 //
 // Bound by memory: a row of d elements is read once and written once (keys and values twice where both a tensor and the cache take
 // them), at some 12 flops per element.  A row is held by d/8 lanes, eight elements each; a wavefront takes 4 (d = 128) or 8 rows
-// of one token at a time, so that the angles, the same for all heads, are made once per lane and token: four of them, the eight elements
-// being four pairs.  With pairs (i, i + rotated/2) a lane holds elements 4j.. and rotated/2 + 4j.., two pieces of 8 bytes, and no
-// element changes lanes; with pairs (2i, 2i + 1) one piece of 16 bytes.  Angles: position * frequency / 2 pi in 64 bits, less its nearest
-// whole number, which at 32 bits would be off by 0.06 of a radian at position 10^6.  Sums, norms and turns are in 32 bits, and there is one
+// of one token at a time, so that the angles, the same for all heads, are made once per token, one by each
+// lane, which then takes the four it turns its four pairs of elements by from other lanes.  With pairs (i, i + rotated/2) a lane holds
+// elements 4j.. and rotated/2 + 4j.., two pieces of 8 bytes, and no element changes lanes; with pairs (2i, 2i + 1) one piece of 16 bytes.
+// Rows are stored non-temporally (2048 tokens of 48 heads 22.8 -> 14.8 us) and loaded a trip ahead.  32 + 2 x 8 heads x 16384 into the cache, 403 MB:
+// 77 us, 5.2 TB/s (a copy of 2 GiB: 4.8).  Angles: position * frequency / 2 pi in 64 bits, less its nearest
+// whole number; in 32 bits it would be off by 0.06 of a radian at position 10^6.  Sums, norms and turns are in 32 bits, and there is one
 // rounding, to the type of the rows.
 namespace sawattn {
 
@@ -63,7 +65,8 @@ __device__ __forceinline__ unsigned narrow(float a, float b) {
     }
 }
 
-template <int D, bool BF16, bool INTERLEAVED>
+// AHEAD: the rows of a trip are on their way while those before are worked on, the first while the angles are made.
+template <int D, bool BF16, bool INTERLEAVED, bool AHEAD>
 __global__ __launch_bounds__(kPrepareThreads) void qkv_prepare_kernel(PrepareParams p) {
     constexpr int kLanes = D / 8, kRows = 64 / kLanes;
     const int lane = threadIdx.x & 63, j = lane % kLanes, group = lane / kLanes;
@@ -78,15 +81,6 @@ __global__ __launch_bounds__(kPrepareThreads) void qkv_prepare_kernel(PreparePar
     // the lane's eight elements, in bytes: two pieces of four, or (one behind the other) one of eight
     const int low = (INTERLEAVED || !turns) ? 16 * j : 8 * j;
     const int high = (INTERLEAVED || !turns) ? 16 * j + 8 : p.rotated + 8 * j;
-    float cosine[4] = {1.f, 1.f, 1.f, 1.f}, sine[4] = {0.f, 0.f, 0.f, 0.f};
-    if (turns) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            double turn = (double)position * p.frequencies[4 * j + i] * 0.15915494309189533577;      // 1 / (2 pi)
-            turn -= __builtin_rint(turn);
-            sincospif(2.f * (float)turn, &sine[i], &cosine[i]);
-        }
-    }
     f4 wq[2], wk[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -113,24 +107,54 @@ __global__ __launch_bounds__(kPrepareThreads) void qkv_prepare_kernel(PreparePar
     char* const k_slot = page >= 0 ? p.cache_k + page * p.k_page + page_row * p.k_row : nullptr;
     char* const v_slot = page >= 0 ? p.cache_v + page * p.v_page + page_row * p.v_row : nullptr;
 
-    const int rows = p.H + 2 * p.KH;
-    for (int trip = 0; trip < p.trips; ++trip) {
-        const int row = (chunk * p.trips + trip) * kRows + group;
-        if (row >= rows) break;
+    const int rows = p.H + 2 * p.KH, row0 = chunk * p.trips * kRows + group;
+    struct Row {
+        bool is_q, is_v;
+        int head;
+    };
+    auto row_of = [&](int row) {
         const bool is_q = row < p.H, is_v = row >= p.H + p.KH;
-        const int head = is_q ? row : is_v ? row - p.H - p.KH : row - p.H;
-        const char* from = is_q ? q + head * p.q.head : is_v ? v + head * p.v.head : k + head * p.k.head;
-        u2 x[2];
+        return Row{is_q, is_v, is_q ? row : is_v ? row - p.H - p.KH : row - p.H};
+    };
+    auto fetch = [&](const Row& row, u2 (&to)[2]) {      // the lane's pieces of it
+        const char* from = row.is_q ? q + row.head * p.q.head : row.is_v ? v + row.head * p.v.head : k + row.head * p.k.head;
         if constexpr (INTERLEAVED) {
-            const u4* at = reinterpret_cast<const u4*>(from + low);
-            const u4 both = *at;
-            x[0] = u2{both[0], both[1]};
-            x[1] = u2{both[2], both[3]};
+            const u4 both = *reinterpret_cast<const u4*>(from + low);
+            to[0] = u2{both[0], both[1]};
+            to[1] = u2{both[2], both[3]};
         } else {
-            const u2* at = reinterpret_cast<const u2*>(from + low);
-            const u2* and_at = reinterpret_cast<const u2*>(from + high);
-            x[0] = *at;
-            x[1] = *and_at;
+            to[0] = *reinterpret_cast<const u2*>(from + low);
+            to[1] = *reinterpret_cast<const u2*>(from + high);
+        }
+    };
+    u2 coming[2] = {};
+    if (AHEAD && row0 < rows) fetch(row_of(row0), coming);
+    // One pair of a cosine and a sine per lane, those of the token's pairs of elements (in both halves of the wavefront at d = 64); a lane then
+    // fetches the four it turns by.  Four per lane of a row cost more code than the rest of the kernel.
+    float cosine[4], sine[4];
+    {
+        const int pair = lane % (D / 2);
+        double turn = pair < p.rotated / 2 ? (double)position * p.frequencies[pair] * 0.15915494309189533577 : 0.;      // 1 / (2 pi)
+        turn -= __builtin_rint(turn);
+        float c, s;
+        sincospif(2.f * (float)turn, &s, &c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            cosine[i] = __shfl(c, 4 * j + i);
+            sine[i] = __shfl(s, 4 * j + i);
+        }
+    }
+    for (int trip = 0; trip < p.trips; ++trip) {
+        const int row = row0 + trip * kRows;
+        if (row >= rows) break;
+        const auto [is_q, is_v, head] = row_of(row);
+        u2 x[2];
+        if constexpr (AHEAD) {
+            x[0] = coming[0];
+            x[1] = coming[1];
+            if (trip + 1 < p.trips && row + kRows < rows) fetch(row_of(row + kRows), coming);
+        } else {
+            fetch(Row{is_q, is_v, head}, x);
         }
         if (!is_v) {
             float y[8];
@@ -178,8 +202,11 @@ __global__ __launch_bounds__(kPrepareThreads) void qkv_prepare_kernel(PreparePar
 
 template <int D, bool BF16>
 void launch_prepare(const PrepareParams& p, bool interleaved, int grid, hipStream_t stream) {
-    if (interleaved) hipLaunchKernelGGL((qkv_prepare_kernel<D, BF16, true>), dim3(grid), dim3(kPrepareThreads), 0, stream, p);
-    else hipLaunchKernelGGL((qkv_prepare_kernel<D, BF16, false>), dim3(grid), dim3(kPrepareThreads), 0, stream, p);
+    // Loading ahead, where there is anything to load ahead: 8192 tokens of 48 heads 49 -> 44 us, 16384 85 -> 77, 4096 28 -> 24, 1024 8.2 -> 7.7; a single
+    // token (one trip) would take 3.3 instead of 3.2.
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(kPrepareThreads), 0, stream, p); };
+    if (interleaved) p.trips > 1 ? launch(qkv_prepare_kernel<D, BF16, true, true>) : launch(qkv_prepare_kernel<D, BF16, true, false>);
+    else p.trips > 1 ? launch(qkv_prepare_kernel<D, BF16, false, true>) : launch(qkv_prepare_kernel<D, BF16, false, false>);
 }
 
 }  // namespace sawattn
@@ -238,8 +265,7 @@ extern "C" int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache*
     p.q_weight = q_weight; p.k_weight = k_weight; p.frequencies = frequencies;
     p.eps = eps; p.rotated = rotated; p.tokens = B * N; p.N = N; p.H = H; p.KH = KH;
     // A wavefront takes all rows of a token, or, where that would make fewer than 4096 wavefronts, fewer of them, 4 (d = 128) or 8 at least.  Measured, 32 +
-    // 2 x 8 heads of 128 into the cache, 2048, 4096, 8192 and 65536 wavefronts: 1024 tokens 9.0, 8.7, 9.7, 10.9 us; 4096 tokens 28.0, 28.2, 28.3, 39.5;
-    // 2048 tokens 14.8, 12.8, 13.7, 19.0.
+    // 2 x 8 heads of 128 into the cache, 2048, 4096 and 8192 wavefronts: 1024 tokens 8.7, 7.6, 7.8 us; 2048 tokens 13.8, 11.5, 12.3; 4096 tokens 24.2, 23.5, 25.0.
     const int heads = H + 2 * KH, at_once = 64 / (d / 8), all = (heads + at_once - 1) / at_once;
     const int wanted = (int)std::min<long long>(all, (4096 + p.tokens - 1) / p.tokens);
     p.trips = (all + wanted - 1) / wanted;

@@ -813,7 +813,7 @@ def test_built_kernels(tmp_path):
     from .util import device_code, device_listing, kernel_bodies, llvm_tool
     notes = llvm_tool("llvm-readelf", "--notes", device_code(tmp_path))
     found = dict(re.findall(r"\.name:\s+(_ZN7sawattn\d+(?:kv_pages|qkv_prepare|decode|decode_join)_kernel\S+)\s+\.private_segment_fixed_size:\s+(\d+)", notes, re.S))
-    assert len(found) >= 2 + 8 + 20 + 2 and set(found.values()) == {"0"}, found
+    assert len(found) >= 2 + 12 + 20 + 2 and set(found.values()) == {"0"}, found
     (tmp_path / "listing").mkdir()
     seen = 0
     for kernel, body in kernel_bodies(device_listing(tmp_path / "listing")).items():
