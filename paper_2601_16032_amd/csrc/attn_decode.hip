@@ -96,7 +96,7 @@ struct DecodeShare {
         if (left <= 0) return;
         const int wanted = (unsigned)at / (unsigned)p.units;
         int before = 0;      // steps of the requests in front
-        for (int r0 = 0;; r0 += 64) {
+        for (int r0 = 0; r0 < p.R; r0 += 64) {
             const int given = r0 == 0 ? given0 : r0 + lane < p.R ? p.lengths[r0 + lane] : 0;
             const int steps = DecodeRequest(p, given).steps, upto = lanes_upto(steps);
             const unsigned long long found = __ballot(before + upto > wanted);
@@ -111,6 +111,7 @@ struct DecodeShare {
             }
             before += __builtin_amdgcn_readlane(upto, 63);
         }
+        left = 0;      // (not reached unless the lengths change meanwhile)
     }
 };
 
@@ -398,15 +399,20 @@ __global__ __launch_bounds__(64 * WAVES, 4) void decode_kernel(DecodeParams p) {
         if (left <= 0) {
             // what is missing of a unit begun here takes the workgroups behind this one, in whole shares
             if (tid == 0)
-                p.begun[blockIdx.x] = int4{t0 == 0 && !whole ? r : -1, unit, workgroup + (request.steps - t1 + share - 1) / max(share, 1), 0};
+                p.begun[blockIdx.x] = int4{t0 == 0 && !whole ? r : -1, unit, min(workgroup + (request.steps - t1 + share - 1) / max(share, 1), p.workgroups - 1), 0};
             return;
         }
         __syncthreads();
         t0 = 0;
-        if (++unit == p.units) {      // (with steps left there is a request left that has some)
+        if (++unit == p.units) {      // (with steps left there is a request left that has some, unless the lengths have changed meanwhile)
             unit = 0;
-            do request = DecodeRequest(p, __builtin_amdgcn_readfirstlane(p.lengths[++r]));
-            while (request.steps == 0);
+            do {
+                if (++r == p.R) {
+                    if (tid == 0) p.begun[blockIdx.x] = int4{-1, 0, 0, 0};
+                    return;
+                }
+                request = DecodeRequest(p, __builtin_amdgcn_readfirstlane(p.lengths[r]));
+            } while (request.steps == 0);
         }
     } while (true);
 }

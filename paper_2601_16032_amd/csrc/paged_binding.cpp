@@ -1,6 +1,6 @@
 // What binding.py does for the operators over a paged key-value cache, where it takes time: looking at a dozen tensors (type, size, device, strides) and
 // handing their addresses to the library.  A decoding step makes these calls once per layer, and in Python the look alone took as long as
-// the launch (attn_kv_pages 3.7 of 7.8 us, attn_qkv_prepare 4.4 of 8.5); here it takes 0.3 us.
+// the launch (attn_kv_pages 3.7 of 7.8 us, attn_qkv_prepare 4.4 of 8.5); here, with the launch, a call takes 4 us.
 //
 // A Python module of three functions that take everything by position and return the library's code; a tensor that does not fit is a ValueError.  The
 // library's functions are handed in (bind), so that there is one copy of it in the process, whoever loaded it.
@@ -83,6 +83,15 @@ float real(PyObject* o) {
 
 void* pointer(PyObject* o) { return o == Py_None ? nullptr : reinterpret_cast<void*>(whole(o)); }
 
+// The library's call, without the interpreter's lock: a launch can wait for room in the queue.
+template <typename F, typename... A>
+int released(F* call, A... args) {
+    PyThreadState* const state = PyEval_SaveThread();
+    const int rc = call(args...);
+    PyEval_RestoreThread(state);
+    return rc;
+}
+
 // Runs `f`, a binding's body: nothing leaves it but a code or a Python error.
 template <typename F>
 PyObject* guarded(Py_ssize_t given, Py_ssize_t wanted, F&& f) {
@@ -135,7 +144,7 @@ PyObject* kv_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (R > INT32_MAX || ring > INT32_MAX || tokens > INT32_MAX) refuse("lengths, free_pages and slots", "of fewer than 2^31 elements");
         const PageTable table(a[2], R, device);
         const auto i32 = [&](int i, const char* name, int64_t size) { return flat<int32_t>(a[i], name, at::kInt, size, device); };
-        return g_kv_pages(i32(0, "lengths", R), i32(1, "new_tokens", R), (int)R, table.at, table.stride, table.wide, small(a[11], "page_size"),
+        return released(g_kv_pages, i32(0, "lengths", R), i32(1, "new_tokens", R), (int)R, table.at, table.stride, table.wide, small(a[11], "page_size"),
                           i32(3, "free_pages", ring), (int)ring, i32(4, "free_state", 2), i32(5, "lengths_out", R), i32(6, "granted", R),
                           i32(7, "token_offsets", R + 1), i32(8, "free_state_out", 2), flat<int64_t>(a[9], "slots", at::kLong, tokens, device),
                           i32(10, "positions", tokens), (int)tokens, pointer(a[12]));
@@ -167,10 +176,12 @@ PyObject* qkv_prepare(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t half = a[13] == Py_None ? 0 : tensor(a[13], "frequencies").numel();
         if (half > INT32_MAX / 2) refuse("frequencies", "of at most d / 2 elements");
         const auto* frequencies = flat<double>(a[13], "frequencies", at::kDouble, half, device, true);
-        return g_qkv_prepare(&all, cache, flat<int64_t>(a[8], "slots", at::kLong, B * N, device, true),
+        const int interleaved = PyObject_IsTrue(a[14]);
+        if (interleaved < 0) throw Refused{};
+        return released(g_qkv_prepare, &all, cache, flat<int64_t>(a[8], "slots", at::kLong, B * N, device, true),
                              flat<int32_t>(a[9], "positions", at::kInt, B * N, device), flat<float>(a[10], "q_weight", at::kFloat, d, device, true),
                              flat<float>(a[11], "k_weight", at::kFloat, d, device, true), real(a[12]), half ? frequencies : nullptr, (int)(2 * half),
-                             PyObject_IsTrue(a[14]) == 1, (int)B, (int)N, (int)H, (int)KH, (int)d, type, pointer(a[15]));
+                             interleaved, (int)B, (int)N, (int)H, (int)KH, (int)d, type, pointer(a[15]));
     });
 }
 
@@ -190,7 +201,7 @@ PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (device_of(workspace) != device || !workspace.is_contiguous()) refuse("workspace", "a contiguous tensor on the other tensors' device");
         const int64_t R = Q.size(0);
         const PageTable table(a[4], R, device);
-        return g_decode(Q.data_ptr(), Q.stride(0), Q.stride(1), O.data_ptr(), O.stride(0), O.stride(1), out, cache, table.at, table.stride, table.wide,
+        return released(g_decode, static_cast<const void*>(Q.data_ptr()), Q.stride(0), Q.stride(1), O.data_ptr(), O.stride(0), O.stride(1), out, cache, table.at, table.stride, table.wide,
                         flat<int32_t>(a[5], "lengths", at::kInt, R, device), (int)R, (int)Q.size(1), real(a[6]), small(a[7], "window"), workspace.data_ptr(),
                         workspace.nbytes(), pointer(a[9]));
     });
