@@ -346,31 +346,21 @@ def _paged_module():
             raise FileNotFoundError(f"{PAGED_BINDING_PATH} is not built; run `python -m paper_2601_16032_amd.build` first")
         L = lib()
         from . import _paged as module
-        module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.attn_kv_pages, L.attn_qkv_prepare, L.attn_decode)))
+        module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.attn_kv_pages, L.attn_qkv_prepare, L.attn_decode, L.hipGetDevice, L.hipSetDevice)))      # (the last two of the HIP runtime it loads)
         _paged = module
     return _paged
 
 
-_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
-
-
-def _on(device, stream, call, *args):
-    """call(*args, handle of the stream or of the device's current one) with `device` current; raises what the library refuses."""
+def _stream_on(device, stream):
+    """Handle of the given stream, or of the device's current one."""
     if device < 0:
         raise ValueError("the first tensor must be a device tensor")
     if stream is None:
-        handle = _current_raw_stream(device)
-    elif stream.device.index == device:
-        handle = stream.cuda_stream
-    else:
+        return _current_raw_stream(device)
+    if stream.device.index != device:
         raise ValueError("the stream must be one of the tensors' device")
-    if device == _current_device():
-        rc = call(*args, handle)
-    else:
-        with torch.cuda.device(device):
-            rc = call(*args, handle)
-    if rc != OK:
-        _check(rc)
+    return stream.cuda_stream
 
 
 def _empty(shape, dtype, device, stream):
@@ -406,8 +396,10 @@ def attn_kv_pages(lengths, new_tokens, table, free_pages, free_state, *, page_si
         lengths_out, granted, token_offsets, free_state_out, positions = (
             _empty(size, torch.int32, lengths.device, stream) if t is None else t for t, size in (
                 (lengths_out, R), (granted, R), (token_offsets, R + 1), (free_state_out, 2), (positions, slots.numel())))
-    _on(lengths.get_device(), stream, (_paged or _paged_module()).kv_pages, lengths, new_tokens, table, free_pages, free_state, lengths_out,
-        granted, token_offsets, free_state_out, slots, positions, page_size)
+    rc = (_paged or _paged_module()).kv_pages(lengths, new_tokens, table, free_pages, free_state, lengths_out, granted, token_offsets,
+                                              free_state_out, slots, positions, page_size, _stream_on(lengths.get_device(), stream))
+    if rc != OK:
+        _check(rc)
     return PageStep(lengths_out, granted, token_offsets, free_state_out, slots, positions)
 
 
@@ -426,8 +418,10 @@ def attn_qkv_prepare(q, k, v, *, positions, frequencies=None, interleaved: bool 
             k_out, v_out = _empty(k.shape, k.dtype, q.device, stream), _empty(k.shape, k.dtype, q.device, stream)
     else:
         ptr, at = cache.ptr, cache.device
-    _on(q.get_device(), stream, (_paged or _paged_module()).qkv_prepare, q, k, v, q_out, k_out, v_out, ptr, at, slots, positions, q_weight,
-        k_weight, eps, frequencies, interleaved)
+    rc = (_paged or _paged_module()).qkv_prepare(q, k, v, q_out, k_out, v_out, ptr, at, slots, positions, q_weight, k_weight, eps, frequencies,
+                                                 interleaved, _stream_on(q.get_device(), stream))
+    if rc != OK:
+        _check(rc)
     return q_out, k_out, v_out
 
 
@@ -448,5 +442,7 @@ def attn_decode(Q, cache: KVCache, table, lengths, O=None, *, scale: float, wind
     if workspace is None:
         workspace = _empty(attn_decode_workspace_bytes(Q.shape[0], Q.shape[1], cache, table.shape[-1]), torch.uint8, Q.device, stream)
     device = cache.device
-    _on(device, stream, (_paged or _paged_module()).decode, Q, O, cache.ptr, device, table, lengths, scale, window, workspace)
+    rc = (_paged or _paged_module()).decode(Q, O, cache.ptr, device, table, lengths, scale, window, workspace, _stream_on(device, stream))
+    if rc != OK:
+        _check(rc)
     return O

@@ -18,6 +18,8 @@ namespace {
 decltype(&attn_kv_pages) g_kv_pages;
 decltype(&attn_qkv_prepare) g_qkv_prepare;
 decltype(&attn_decode) g_decode;
+int (*g_get_device)(int*);      // hipGetDevice, hipSetDevice
+int (*g_set_device)(int);
 
 struct Refused {};      // an error is set
 
@@ -83,12 +85,19 @@ float real(PyObject* o) {
 
 void* pointer(PyObject* o) { return o == Py_None ? nullptr : reinterpret_cast<void*>(whole(o)); }
 
-// The library's call, without the interpreter's lock: a launch can wait for room in the queue.
+// The library's call with `device` current, without the interpreter's lock: a launch can wait for room in the queue.
 template <typename F, typename... A>
-int released(F* call, A... args) {
+int launch(int device, F* call, A... args) {
     PyThreadState* const state = PyEval_SaveThread();
-    const int rc = call(args...);
+    int before = -1, rc = SAWATTN_ERR_RUNTIME;
+    const bool there = g_get_device(&before) == 0 && (before == device || g_set_device(device) == 0);
+    if (there) rc = call(args...);
+    if (before != device && before >= 0) (void)g_set_device(before);
     PyEval_RestoreThread(state);
+    if (!there) {
+        PyErr_Format(PyExc_RuntimeError, "device %d cannot be made current", device);
+        throw Refused{};
+    }
     return rc;
 }
 
@@ -113,14 +122,14 @@ PyObject* guarded(Py_ssize_t given, Py_ssize_t wanted, F&& f) {
     }
 }
 
-// bind(addresses of attn_kv_pages, attn_qkv_prepare, attn_decode)
+// bind(addresses of attn_kv_pages, attn_qkv_prepare, attn_decode, hipGetDevice, hipSetDevice)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 3) {
-        PyErr_SetString(PyExc_TypeError, "three addresses expected");
+    if (n != 5) {
+        PyErr_SetString(PyExc_TypeError, "five addresses expected");
         return nullptr;
     }
-    void* p[3];
-    for (int i = 0; i < 3; ++i) {
+    void* p[5];
+    for (int i = 0; i < 5; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a null address");
@@ -130,6 +139,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g_kv_pages = reinterpret_cast<decltype(g_kv_pages)>(p[0]);
     g_qkv_prepare = reinterpret_cast<decltype(g_qkv_prepare)>(p[1]);
     g_decode = reinterpret_cast<decltype(g_decode)>(p[2]);
+    g_get_device = reinterpret_cast<decltype(g_get_device)>(p[3]);
+    g_set_device = reinterpret_cast<decltype(g_set_device)>(p[4]);
     Py_RETURN_NONE;
 }
 
@@ -144,7 +155,7 @@ PyObject* kv_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (R > INT32_MAX || ring > INT32_MAX || tokens > INT32_MAX) refuse("lengths, free_pages and slots", "of fewer than 2^31 elements");
         const PageTable table(a[2], R, device);
         const auto i32 = [&](int i, const char* name, int64_t size) { return flat<int32_t>(a[i], name, at::kInt, size, device); };
-        return released(g_kv_pages, i32(0, "lengths", R), i32(1, "new_tokens", R), (int)R, table.at, table.stride, table.wide, small(a[11], "page_size"),
+        return launch(device, g_kv_pages, i32(0, "lengths", R), i32(1, "new_tokens", R), (int)R, table.at, table.stride, table.wide, small(a[11], "page_size"),
                           i32(3, "free_pages", ring), (int)ring, i32(4, "free_state", 2), i32(5, "lengths_out", R), i32(6, "granted", R),
                           i32(7, "token_offsets", R + 1), i32(8, "free_state_out", 2), flat<int64_t>(a[9], "slots", at::kLong, tokens, device),
                           i32(10, "positions", tokens), (int)tokens, pointer(a[12]));
@@ -178,7 +189,7 @@ PyObject* qkv_prepare(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const auto* frequencies = flat<double>(a[13], "frequencies", at::kDouble, half, device, true);
         const int interleaved = PyObject_IsTrue(a[14]);
         if (interleaved < 0) throw Refused{};
-        return released(g_qkv_prepare, &all, cache, flat<int64_t>(a[8], "slots", at::kLong, B * N, device, true),
+        return launch(device, g_qkv_prepare, &all, cache, flat<int64_t>(a[8], "slots", at::kLong, B * N, device, true),
                              flat<int32_t>(a[9], "positions", at::kInt, B * N, device), flat<float>(a[10], "q_weight", at::kFloat, d, device, true),
                              flat<float>(a[11], "k_weight", at::kFloat, d, device, true), real(a[12]), half ? frequencies : nullptr, (int)(2 * half),
                              interleaved, (int)B, (int)N, (int)H, (int)KH, (int)d, type, pointer(a[15]));
@@ -201,7 +212,7 @@ PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (device_of(workspace) != device || !workspace.is_contiguous()) refuse("workspace", "a contiguous tensor on the other tensors' device");
         const int64_t R = Q.size(0);
         const PageTable table(a[4], R, device);
-        return released(g_decode, static_cast<const void*>(Q.data_ptr()), Q.stride(0), Q.stride(1), O.data_ptr(), O.stride(0), O.stride(1), out, cache, table.at, table.stride, table.wide,
+        return launch(device, g_decode, static_cast<const void*>(Q.data_ptr()), Q.stride(0), Q.stride(1), O.data_ptr(), O.stride(0), O.stride(1), out, cache, table.at, table.stride, table.wide,
                         flat<int32_t>(a[5], "lengths", at::kInt, R, device), (int)R, (int)Q.size(1), real(a[6]), small(a[7], "window"), workspace.data_ptr(),
                         workspace.nbytes(), pointer(a[9]));
     });
