@@ -402,7 +402,7 @@ int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache* cache, con
  *   strides            in elements, not negative, multiples of 8
  *   cache              host struct, read during the call; row strides at most 2^26
  *   table              device, read: int32 [R] rows of max_pages >= 1 entries, table_stride apart; max_pages*page_size at most 2^30,
- *                      R*H*ceil(max_pages*page_size/128) below 2^31 - 2048.
+ *                      R*cache->heads*ceil(max_pages*page_size/128) below 2^31 - 2048.
  *                      Entries behind the length's pages are not read as pages.
  *   lengths            device, read: int32 [R]; above max_pages*page_size they count as that, below 0 as 0
  *   R, H               >= 1, R*H below 2^22; H a multiple of cache->heads.  Up to 16 query heads share one reading of their keys and

@@ -511,7 +511,7 @@ int decode_plan(const sawattn_kv_cache* cache, int R, int H, int max_pages, int 
     out->seen = (int)(window > 0 ? std::min<long long>(capacity, window) : capacity);
     const double most = (double)R * out->units * ((capacity + kDecodeStep - 1) / kDecodeStep);      // steps
     if (most >= 2147483648.0 - 2.0 * kDecodeGrid)
-        return fail(SAWATTN_ERR_INVALID_ARG, "R*H*ceil(max_pages*page_size/128) must be below 2^31 - 2048");
+        return fail(SAWATTN_ERR_INVALID_ARG, "R*heads*ceil(max_pages*page_size/128) must be below 2^31 - 2048");
     // One workgroup reads about 55 GB/s, the second kernel costs 6 us and more.  Few units: up to 500 keys at d = 128 take 8.5 us in one launch,
     // in two 9; 1000 keys 12.5 and 9.4.  Units for every compute unit and more: 256 requests of 1000 keys, 8 heads: 170 and 190 us, 128 ragged
     // requests up to 2000: 57 and 62.

@@ -358,6 +358,33 @@ def test_prepare_in_place_and_by_rows(interleaved):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("d,H,KH", [(128, 7, 2), (64, 13, 5)])
+def test_prepare_several_trips(d, H, KH, interleaved):
+    """Enough tokens for a wavefront to take a token's rows in several trips, the last not full; in place, with padding among them, into a cache."""
+    N, ps = 5000, 32
+    q, k, v, (wq, wk) = prepare_inputs(1, N, H, KH, d, "bf16", seed=6)
+    pos = torch.arange(N, dtype=torch.int32, device="cuda")
+    pos[[3, 77, 4999]] = -1
+    slots = torch.randperm((N // ps + 2) * ps, generator=torch.Generator().manual_seed(5))[:N].cuda()
+    kw = dict(positions=pos, frequencies=frequencies(d // 2), interleaved=interleaved, q_weight=wq, k_weight=wk)
+    pages = [torch.zeros(N // ps + 2, KH, ps, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    outs = [torch.zeros_like(x, memory_format=torch.contiguous_format) for x in (q, k, v)]
+    binding.attn_qkv_prepare(q, k, v, q_out=outs[0], k_out=outs[1], v_out=outs[2], cache=binding.KVCache(*pages), slots=slots, **kw)
+    real = (pos >= 0).cpu().numpy()
+    for got, x, w in ((outs[0], q, wq), (outs[1], k, wk)):
+        exact, size = po.rows(f64(x), f64(w), 1e-6, pos.cpu().numpy(), f64(kw["frequencies"]), interleaved)
+        check_rows(got[:, real], exact[:, real], size[:, real], torch.bfloat16)
+        assert (got[:, ~real] == 0).all()
+    for page, out in zip(pages, outs[1:]):
+        assert torch.equal(page.transpose(1, 2).reshape(-1, KH, d)[slots], out[0])
+    untouched = [x[:, ~real].clone() for x in (q, k, v)]
+    binding.attn_qkv_prepare(q, k, v, q_out=q, k_out=k, v_out=v, **kw)
+    for x, out, kept in zip((q, k, v), outs, untouched):
+        assert torch.equal(x[:, real], out[:, real]) and torch.equal(x[:, ~real], kept)
+
+
+@pytest.mark.gpu
 def test_prepare_many_tokens():
     """More tokens than one round of wavefronts, and offsets that pass 32 bits (the last row at 2^32 bytes and more)."""
     B, N, H, KH, d = 2, 3001, 6, 2, 64
