@@ -233,9 +233,14 @@ struct DecodeState {
                 }
             }
         };
-        if (BRIEF && edge) load(std::false_type{});
-        else load(std::true_type{});
-        wait_tile_landed();
+        if (BRIEF && edge) {
+            load(std::false_type{});
+            wait_tile_landed();
+        } else {
+            load(std::true_type{});
+            // K has landed when no more are on their way than the eight loads of V behind it (1 x 200 keys 4.08 -> 3.93 us, 64 ragged 94 -> 92.7)
+            asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        }
         f4 s[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
         for (int x = 0; x < D / 32; ++x)
