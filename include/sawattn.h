@@ -404,6 +404,8 @@ int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache* cache, con
  *   table              device, read: int32 [R] rows of max_pages >= 1 entries, table_stride apart; max_pages*page_size at most 2^30,
  *                      R*cache->heads*ceil(max_pages*page_size/128) below 2^31 - 2048.
  *                      Entries behind the length's pages are not read as pages.
+ *                      max_pages bounds what the launch has to be ready for: a host that knows its longest request passes the pages of that one
+ *                      (table_stride stays) and may be spared the second kernel.
  *   lengths            device, read: int32 [R]; above max_pages*page_size they count as that, below 0 as 0
  *   R, H               >= 1, R*H below 2^22; H a multiple of cache->heads.  Up to 16 query heads share one reading of their keys and
  *                      values, more read them once per 16.
