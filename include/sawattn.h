@@ -416,7 +416,7 @@ int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache* cache, con
  * A request of length 0 gets zeros.  A row of the cache outside the visible ones is never used, whatever it holds; an infinity among the visible
  * values makes the elements it meets NaN.  A table entry outside
  * 0 .. pages - 1 among the visible ones makes the request's O NaN.  Products are exact, scores, probabilities, sums and O are held in 32 bits
- * (the probabilities enter the second product as sums of two 16-bit numbers).  The result does not depend on timing.
+ * (the probabilities enter the second product as sums of 16-bit numbers, 22 bits in all at binary16, 24 at bfloat16).  The result does not depend on timing.
  * One launch where the rows that can be visible are few (up to 256 KiB of K and V per request and key/value head, or 1 MiB with
  * 256 of those and more), else two.  Stream and errors as attn_fwd.
  */

@@ -21,8 +21,8 @@
 // of each per lane, four whole rows per load, and never leaves the registers: pairs of rows are interleaved (v_perm) into A operands, whose MFMA j
 // has elements j, j + D/16, ... of V.
 //
-// The probabilities enter the second product as the sum of two 16-bit numbers, so that they are not rounded: the matrix cores have time
-// for both.  Binary16 ones are scaled by 2^12 for the sake of small ones.
+// The probabilities enter the second product as sums of 16-bit numbers, for which the matrix cores have time: bfloat16 ones of three, which
+// hold all 24 bits, binary16 ones of two, which hold 22, scaled by 2^12 for the sake of small ones.
 //
 // K and V are read with non-temporal loads (7.1 instead of 6.3 TB/s for a kernel that only reads).  Measured with the products taken out,
 // the loads of 16 x 32768 take 655 us (pages of 16 rows in any order; of 256 rows: 645), with them 660: 6.5 TB/s.  Loading a tile ahead, in
@@ -120,6 +120,27 @@ __device__ __forceinline__ f4 decode_mfma(u4 a, u4 b, f4 c) {
     if constexpr (BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
 }
+
+// Two probabilities as 16-bit numbers that add up to them: what each leaves goes to the next.
+template <bool BF16>
+struct DecodePieces {
+    static constexpr int kCount = BF16 ? 3 : 2;
+    unsigned word[kCount];
+    __device__ __forceinline__ DecodePieces(float a, float b) {
+        if constexpr (BF16) {      // cut off, eight bits of 24 at a time: exact
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) {
+                const unsigned x = __builtin_bit_cast(unsigned, a), y = __builtin_bit_cast(unsigned, b);
+                word[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                a -= __builtin_bit_cast(float, x & 0xffff0000u);
+                b -= __builtin_bit_cast(float, y & 0xffff0000u);
+            }
+        } else {
+            word[0] = narrow<false>(a, b);
+            word[1] = narrow<false>(a - widen<false>(word[0], 0), b - widen<false>(word[0], 1));
+        }
+    }
+};
 
 // The larger, and the sum, of x in the four lanes that hold a head.
 __device__ __forceinline__ void lane_quarters(float x, float& one, float& other) {      // neighbouring rows of 16 lanes exchanged
@@ -272,21 +293,23 @@ struct DecodeState {
         }
         // (nothing seen so far: any finite reference gives probabilities of 0)
         const float reference = (m == -INFINITY ? 0.f : m) - (BF16 ? 0.f : 12.f);
-        u4 high, rest;
+        using Pieces = DecodePieces<BF16>;
+        u4 piece[Pieces::kCount];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const float a = fast_exp2(s[w / 2][w % 2 * 2] - reference), b = fast_exp2(s[w / 2][w % 2 * 2 + 1] - reference);
             l += a + b;
-            high[w] = narrow<BF16>(a, b);
-            rest[w] = narrow<BF16>(a - widen<BF16>(high[w], 0), b - widen<BF16>(high[w], 1));
+            const Pieces pieces(a, b);
+#pragma unroll
+            for (int i = 0; i < Pieces::kCount; ++i) piece[i][w] = pieces.word[i];
         }
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
             u4 a;      // element j of the lane's pieces of its eight rows
 #pragma unroll
             for (int w = 0; w < 4; ++w) a[w] = __builtin_amdgcn_perm(v[2 * w + 1][j / 2], v[2 * w][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-            o[j] = decode_mfma<BF16>(a, high, o[j]);
-            o[j] = decode_mfma<BF16>(a, rest, o[j]);
+#pragma unroll
+            for (int i = 0; i < Pieces::kCount; ++i) o[j] = decode_mfma<BF16>(a, piece[i], o[j]);
         }
     }
 };

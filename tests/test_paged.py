@@ -890,3 +890,40 @@ def test_steps_study_runs(capsys):
     exact, size = po.rows(f64(held["qkv"][:, 6:9]), np.ones(64), 1e-6, np.full(3, 128), f64(held["frequencies"]), False)
     check_rows(torch.stack([k[128] for k in keys[0]]), exact, size, torch.float16)
     assert all(torch.equal(v[128], held["qkv"][r, 9:]) for r, v in enumerate(keys[1]))
+
+
+# ------------------------------------------------------------------------------------------- what a probability holds
+
+def weighed(R, d, dtype, wide):
+    """R requests of two keys and one head: scores 0 and -x, values 0 and 1, x every number of `dtype` in turn from 1/4 on, below 2.
+    O = p / (1 + p), p = exp(-x)."""
+    step = torch.finfo(DTYPES[dtype]).eps
+    per = int(1 / step)
+    i = np.linspace(0, 3 * per - 1, R).astype(np.int64)
+    x = 2.0 ** (i // per - 2) * (1 + i % per * step)
+    k, v = (torch.zeros(R, 1, 16, d, dtype=DTYPES[dtype], device="cuda") for _ in range(2))
+    k[:, 0, 1, 3] = -torch.tensor(x, device="cuda").to(DTYPES[dtype])
+    assert np.array_equal(-f64(k[:, 0, 1, 3]), x)
+    v[:, 0, 1] = 1.0
+    q = torch.zeros(R, 1, d, dtype=DTYPES[dtype], device="cuda")
+    q[:, :, 3] = 1.0
+    table = torch.full((R, wide), POISON, dtype=torch.int32, device="cuda")
+    table[:, 0] = torch.arange(R, dtype=torch.int32, device="cuda")
+    return q, binding.KVCache(k, v), table, np.exp(-x)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("wide", [1, 400])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_decode_probabilities_in_32_bits(dtype, d, wide):
+    """Off by 2^-20 at most, relative: the operand of exp2 is 2.9 at most and rounded twice (constant and product, 2^-24 each: 2^-22 of the
+    probability), exp2 one unit in the last place (2^-23), the second product three additions (2^-23 each), the sum and the quotient one unit.
+    Probabilities in 16 bits are off by 2^-17."""
+    R = 384
+    q, cache, table, p = weighed(R, d, dtype, wide)
+    assert (binding.attn_decode_workspace_bytes(R, 1, cache, wide) > 0) == (wide == 400)
+    got = f64(binding.attn_decode(q, cache, table, torch.full((R,), 2, dtype=torch.int32, device="cuda"), scale=1.0, o_dtype=torch.float32))
+    want = (p / (1 + p))[:, None, None]
+    off = np.abs(got - want) / want
+    assert off.max() <= 2.0 ** -20, math.log2(off.max())
