@@ -413,10 +413,10 @@ int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache* cache, con
  *   window             >= 0; only rows lengths[r] - window and later are visible; 0: all
  *   workspace          device, written, 16-byte aligned, of at least attn_decode_workspace_bytes (NULL where that is 0); used by this call's kernels only, so
  *                      calls that overlap in time need one each.  Nothing in it has to start out zero.
- * A request of length 0 gets zeros.  A row of the cache outside the visible ones is never used, whatever it holds; an infinity among the visible
- * values makes the elements it meets NaN.  A table entry outside
- * 0 .. pages - 1 among the visible ones makes the request's O NaN.  Products are exact, scores, probabilities, sums and O are held in 32 bits
- * (the probabilities enter the second product as sums of 16-bit numbers, 22 bits in all at binary16, 24 at bfloat16).  The result does not depend on timing.
+ * A request of length 0 gets zeros.  A row of the cache outside the visible ones is never used, whatever it holds.  An infinity among the visible
+ * values makes the elements it meets infinite (NaN where there is one of either sign), NaN if its probability is less than 2^-38 of the largest.
+ * A table entry outside 0 .. pages - 1 among the visible ones makes the request's O NaN.  Products are exact, scores, probabilities, sums and O are held
+ * in 32 bits (the probabilities enter the second product as sums of three 16-bit numbers).  The result does not depend on timing.
  * One launch where the rows that can be visible are few (up to 256 KiB of K and V per request and key/value head, or 1 MiB with
  * 256 of those and more), else two.  Stream and errors as attn_fwd.
  */

@@ -21,8 +21,8 @@
 // of each per lane, four whole rows per load, and never leaves the registers: pairs of rows are interleaved (v_perm) into A operands, whose MFMA j
 // has elements j, j + D/16, ... of V.
 //
-// The probabilities enter the second product as sums of 16-bit numbers, for which the matrix cores have time: bfloat16 ones of three, which
-// hold all 24 bits, binary16 ones of two, which hold 22, scaled by 2^12 for the sake of small ones.
+// The probabilities enter the second product as sums of three 16-bit numbers (DecodePieces), for which the matrix cores have time.  Binary16 ones are
+// scaled by 2^15 for the sake of small ones.
 //
 // K and V are read with non-temporal loads (7.1 instead of 6.3 TB/s for a kernel that only reads).  Measured with the products taken out,
 // the loads of 16 x 32768 take 655 us (pages of 16 rows in any order; of 256 rows: 645), with them 660: 6.5 TB/s.  Loading a tile ahead, in
@@ -121,23 +121,24 @@ __device__ __forceinline__ f4 decode_mfma(u4 a, u4 b, f4 c) {
     else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
 }
 
-// Two probabilities as 16-bit numbers that add up to them: what each leaves goes to the next.
+// Two probabilities as sums of three 16-bit numbers each: cut off, not rounded, and what each leaves goes to the next, which holds all of their 24 bits
+// (binary16: down to 2^-16 of the largest, below that to 2^-38 of it).  None of the three is zero or negative unless the probability is that
+// small: the product of such a one with an infinite value would be no number, or the other infinity.
 template <bool BF16>
 struct DecodePieces {
-    static constexpr int kCount = BF16 ? 3 : 2;
+    static constexpr int kCount = 3;
     unsigned word[kCount];
     __device__ __forceinline__ DecodePieces(float a, float b) {
-        if constexpr (BF16) {      // cut off, eight bits of 24 at a time: exact
+        constexpr float kLeast = BF16 ? 0x1p-100f : 0x1p-24f;
+        const float least_a = fminf(a, kLeast), least_b = fminf(b, kLeast);
 #pragma unroll
-            for (int i = 0; i < kCount; ++i) {
-                const unsigned x = __builtin_bit_cast(unsigned, a), y = __builtin_bit_cast(unsigned, b);
-                word[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-                a -= __builtin_bit_cast(float, x & 0xffff0000u);
-                b -= __builtin_bit_cast(float, y & 0xffff0000u);
+        for (int i = 0; i < kCount; ++i) {
+            if (i) {
+                a = fmaxf(a - widen<BF16>(word[i - 1], 0), least_a);
+                b = fmaxf(b - widen<BF16>(word[i - 1], 1), least_b);
             }
-        } else {
-            word[0] = narrow<false>(a, b);
-            word[1] = narrow<false>(a - widen<false>(word[0], 0), b - widen<false>(word[0], 1));
+            if constexpr (BF16) word[i] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
+            else word[i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(a, b));
         }
     }
 };
@@ -292,7 +293,7 @@ struct DecodeState {
             for (int j = 0; j < D / 16; ++j) o[j] *= fade;
         }
         // (nothing seen so far: any finite reference gives probabilities of 0)
-        const float reference = (m == -INFINITY ? 0.f : m) - (BF16 ? 0.f : 12.f);
+        const float reference = (m == -INFINITY ? 0.f : m) - (BF16 ? 0.f : 15.f);
         using Pieces = DecodePieces<BF16>;
         u4 piece[Pieces::kCount];
 #pragma unroll

@@ -927,3 +927,41 @@ def test_decode_probabilities_in_32_bits(dtype, d, wide):
     want = (p / (1 + p))[:, None, None]
     off = np.abs(got - want) / want
     assert off.max() <= 2.0 ** -20, math.log2(off.max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d,length", [(64, 300), (128, 300), (64, 6000), (128, 6000)])
+def test_decode_infinite_values(dtype, d, length):
+    """An infinity among the visible values makes the elements it meets infinite; one of either sign makes them NaN; no other element changes."""
+    inf, lengths = float("inf"), [length] * 4
+    cache, table, keys = fill_cache(lengths, 2, d, 16, dtype, seed=length + d)
+    for r, at, head, e, x in ((0, 0, 0, 3, inf), (0, 150, 1, 60, -inf), (1, length - 1, 0, 5, -inf), (1, 7, 0, 5, -inf), (2, 40, 0, 9, inf),
+                              (2, 290, 0, 9, -inf), (2, 33, 1, 0, inf), (2, 34, 1, 1, -inf)):
+        cache.v[int(table[r, at // 16]), head, at % 16, e] = keys[1][r][at, head, e] = x
+    q, lens = queries(4, 6, d, dtype, seed=4), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    for out in (q.dtype, torch.float32):
+        got = binding.attn_decode(q, cache, table, lens, scale=d ** -0.5, o_dtype=out)
+        with np.errstate(invalid="ignore"):
+            exact, _, _ = po.decode(f64(q), *[[f64(x) for x in side] for side in keys], d ** -0.5, lengths)
+        assert np.isinf(exact).sum() == 5 * 3 and np.isnan(exact).sum() == 3
+        odd = ~np.isfinite(exact)
+        assert np.array_equal(f64(got)[odd], exact[odd], equal_nan=True)
+        plain = [[torch.where(x.isinf(), 0, x) for x in side] for side in keys]
+        without = torch.where(torch.tensor(odd, device="cuda"), 0, got)
+        bound_by = binding.KVCache(cache.k, torch.where(cache.v.isinf(), 0, cache.v))
+        same = binding.attn_decode(q, bound_by, table, lens, scale=d ** -0.5, o_dtype=out)
+        assert torch.equal(torch.where(torch.tensor(odd, device="cuda"), 0, same), without)
+        check_decode(same, q, plain, d ** -0.5, lengths)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("wide", [1, 400])
+def test_decode_infinite_values_of_small_weight(dtype, wide):
+    """Probabilities down to 2^-38 of the largest: e^-26 = 2^-37.5."""
+    q, cache, table, _ = weighed(300, 128, dtype, wide)
+    cache.k[:, 0, 1, 3] = -torch.linspace(0, 26, 300, device="cuda").to(q.dtype)
+    cache.v[:, 0, 1], cache.v[150:, 0, 1] = float("inf"), float("-inf")
+    got = binding.attn_decode(q, cache, table, torch.full((300,), 2, dtype=torch.int32, device="cuda"), scale=1.0)
+    assert (got[:150] == float("inf")).all() and (got[150:] == float("-inf")).all()
