@@ -426,7 +426,7 @@ def attn_qkv_prepare(q, k, v, *, positions, frequencies=None, interleaved: bool 
 
 
 def attn_decode_workspace_bytes(R: int, H: int, cache: KVCache, max_pages: int) -> int:
-    """Bytes of workspace attn_decode needs for R requests of H heads and page tables of max_pages entries."""
+    """Bytes of workspace attn_decode needs for R requests of H heads, or fewer requests, and page tables of max_pages entries, or fewer."""
     n = ctypes.c_size_t(0)
     _check(lib().attn_decode_workspace_bytes(cache.ptr, R, H, max_pages, ctypes.byref(n)))
     return int(n.value)

@@ -587,6 +587,13 @@ int attn_decode_workspace_bytes(const sawattn_kv_cache* cache, int R, int H, int
     DecodePlan plan;
     rc = decode_plan(cache, R, H, max_pages, 0, &plan);
     if (rc != SAWATTN_OK) return rc;
+    // Enough for smaller batches too.  The need rises with R and max_pages while units are shared; where there are so many of them that they are not, it is
+    // that of the largest batch for which they are.
+    const int shared = (int)std::min<long long>(R, (kDecodeUnits - 1) / ((long long)plan.units * plan.head_groups));
+    if (plan.direct && shared > 0) {
+        rc = decode_plan(cache, shared, H, max_pages, 0, &plan);
+        if (rc != SAWATTN_OK) return rc;
+    }
     *bytes = decode_bytes(plan, cache->d);
     return SAWATTN_OK;
 }

@@ -965,3 +965,30 @@ def test_decode_infinite_values_of_small_weight(dtype, wide):
     cache.v[:, 0, 1], cache.v[150:, 0, 1] = float("inf"), float("-inf")
     got = binding.attn_decode(q, cache, table, torch.full((300,), 2, dtype=torch.int32, device="cuda"), scale=1.0)
     assert (got[:150] == float("inf")).all() and (got[150:] == float("-inf")).all()
+
+
+# ------------------------------------------------------------------------------------------- workspaces
+
+def workspace_bytes(cache, R, H, pages):
+    n = ctypes.c_size_t(0)
+    assert binding.lib().attn_decode_workspace_bytes(ctypes.addressof(cache), R, H, pages, ctypes.byref(n)) == 0, binding.attn_last_error()
+    return n.value
+
+
+@pytest.mark.parametrize("d,KH,H,ps", [(128, 8, 32, 16), (64, 8, 8, 64), (128, 2, 96, 16), (64, 1, 1, 16), (128, 1, 260, 32)])
+def test_decode_workspace_of_the_largest_batch(d, KH, H, ps):
+    """What is reported for a batch and a table does for every smaller batch and table, at any window.  The calls name the same memory for O and
+    Q: they are refused for that once they have found the workspace large enough."""
+    cache = cache_struct(d=d, heads=KH, page_size=ps, k=0x100000000, v=0x200000000, k_page=KH * ps * d, k_head=ps * d, k_row=d, v_page=KH * ps * d,
+                         v_head=ps * d, v_row=d)
+    L, batches, tables = binding.lib(), (1, 2, 7, 31, 32, 33, 63, 255, 256, 300), (1, 17, 128, 200, 1000)
+    for R in batches:
+        for pages in tables:
+            most = workspace_bytes(cache, R, H, pages)
+            for fewer in (r for r in batches if r <= R):
+                for narrower in (p for p in tables if p <= pages):
+                    assert workspace_bytes(cache, fewer, H, narrower) <= most
+                    for window in (0, 300):
+                        rc = L.attn_decode(0x1000000, H * d, d, 0x1000000, H * d, d, 0, ctypes.addressof(cache), 0x3000000, narrower, narrower,
+                                           0x4000000, fewer, H, 0.1, window, 0x5000000, most, None)
+                        refused(rc, binding.ERR_INVALID_ARG, "must not overlap what is read")
