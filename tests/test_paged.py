@@ -992,3 +992,126 @@ def test_decode_workspace_of_the_largest_batch(d, KH, H, ps):
                         rc = L.attn_decode(0x1000000, H * d, d, 0x1000000, H * d, d, 0, ctypes.addressof(cache), 0x3000000, narrower, narrower,
                                            0x4000000, fewer, H, 0.1, window, 0x5000000, most, None)
                         refused(rc, binding.ERR_INVALID_ARG, "must not overlap what is read")
+
+
+class LongServer(Server):
+    """A server whose tables are long enough for units in parts: shares, records of begun units and the second kernel.  Before each step the
+    workspace, made for the largest batch, is filled with bytes that are no number, no request and no place."""
+
+    def __init__(self, **kw):
+        super().__init__(**{"wide": 128, "H": 40, "d": 128, "dtype": "bf16", **kw})      # 20 query heads to a key head: two sets of workgroups
+        assert self.workspace.numel() > 0
+
+    def step(self, qkv, tokens):
+        self.workspace.fill_(0xff)
+        return super().step(qkv, tokens)
+
+
+LONG_PLAN = [[700, 1, 0, 1290, 128, 127], [1, 1, 600, 1, 1, 1], [1, 1, 1, -1, 129, 1], [1, 0, 1, 1500, 1, -1], [1, 1, 1, 1, -1, 0]]
+
+
+@pytest.mark.gpu
+def test_long_steps_of_a_server():
+    """Requests that start, grow over several steps of 128 rows, end and start anew, in parts, against 64 bits."""
+    s = LongServer()
+    for i, new in enumerate(LONG_PLAN):
+        s.new.copy_(torch.tensor(new, dtype=torch.int32))
+        tokens = sum(max(n, 0) for n in new) + 2
+        qkv = queries(tokens, s.H + 2 * s.KH, s.d, s.dtype, seed=200 + i)
+        o, last = s.step(qkv, tokens)
+        torch.cuda.synchronize()
+        lengths = s.host(qkv, new)
+        assert s.lengths.tolist() == lengths
+        s.check(o, last, lengths)
+
+
+@pytest.mark.gpu
+def test_long_steps_captured():
+    """A step in parts captured once and replayed while shares change with the lengths, with eager work in between: the eager results bit by bit."""
+    a, b = LongServer(), LongServer()
+    n = 6 * 300
+    qkv = torch.zeros(n, a.H + 2 * a.KH, a.d, dtype=torch.bfloat16, device="cuda")
+    a.step(qkv, n)      # loads everything, adds nothing
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        o, _ = a.step(qkv, n)
+    for i, new in enumerate([[300, 3, 129, 255, 1, 600], [1] * 6, [300] * 6, [1, -1, 1, 300, 0, -1], [300] * 6, [1] * 6]):
+        for s in (a, b):
+            s.new.copy_(torch.tensor(new, dtype=torch.int32))
+        qkv.copy_(queries(n, a.H + 2 * a.KH, a.d, "bf16", seed=i))
+        graph.replay()
+        torch.cuda.synchronize()
+        want, last = b.step(qkv, n)
+        torch.cuda.synchronize()
+        assert torch.equal(o, want) and a.lengths.tolist() == b.lengths.tolist(), i
+        b.check(want, last, b.host(qkv, new))
+    assert max(b.lengths.tolist()) > 1000
+
+
+@pytest.mark.gpu
+def test_long_steps_on_streams_of_their_own():
+    """Steps in parts on two streams at once, each with its own workspace, and the stream argument: the results of one after the other."""
+    servers, plain = [LongServer(seed=i) for i in (1, 2)], [LongServer(seed=i) for i in (1, 2)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    inputs = [queries(4000, 44, 128, "bf16", seed=i) for i in range(2)]
+    new = torch.tensor([900, 3, 0, 1299, 1, 1700], dtype=torch.int32, device="cuda")
+    for s in servers + plain:
+        s.new.copy_(new)
+    want = [s.step(x, 4000) for s, x in zip(plain, inputs)]
+    torch.cuda.synchronize()
+    assert all(s.lengths.tolist() == new.tolist() for s in plain)
+    got = []
+    for _ in range(4):
+        for s, stream, x in zip(servers, streams, inputs):
+            with torch.cuda.stream(stream):
+                s.lengths.zero_()
+                s.state.copy_(torch.tensor([5, s.ring.numel()], dtype=torch.int32))
+                got.append(s.step(x, 4000)[0])
+    torch.cuda.synchronize()
+    for i, o in enumerate(got):
+        assert torch.equal(o, want[i % 2][0]), i
+    # calls given their streams, queued beside each other
+    outs = [[torch.zeros_like(want[0][0]) for _ in range(4)] for _ in range(2)]
+    for s in servers:
+        s.workspace.fill_(0xff)
+    torch.cuda.synchronize()
+    for j in range(4):
+        for i, s in enumerate(servers):
+            binding.attn_decode(want[i][1], s.cache, s.table, s.lengths, outs[i][j], scale=128 ** -0.5, workspace=s.workspace, stream=streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(o, want[i][0]) for o in outs[i])
+
+
+@pytest.mark.gpu
+def test_decode_one_workspace_for_all():
+    """One workspace, made for the largest batch, used in turn by smaller ones, narrower tables, windows and other numbers of heads, each
+    finding what the one before left: the bits of a call with a workspace of its own."""
+    lengths = [5000, 0, 130, 2048, 1, 4097, 900, 3333] + [37 * i % 300 for i in range(32)]
+    cache, table, keys = fill_cache(lengths, 8, 128, 64, "f16", seed=31)
+    assert binding.attn_decode_workspace_bytes(40, 32, cache, 32) >= binding.attn_decode_workspace_bytes(31, 32, cache, 32) > 0
+    workspace = torch.full((max(binding.attn_decode_workspace_bytes(40, H, cache, table.shape[1]) for H in (32, 8, 160)),), 0xff, dtype=torch.uint8, device="cuda")
+    for R, H, wide, window in ((40, 32, 79, 0), (3, 32, 79, 0), (31, 32, 32, 0), (32, 32, 32, 0), (8, 160, 79, 0), (40, 8, 79, 2500), (1, 8, 79, 0), (6, 32, 79, 1)):
+        q = queries(R, H, 128, "f16", seed=R)
+        seen = [min(n, wide * 64) for n in lengths[:R]]
+        lens = torch.tensor(lengths[:R], dtype=torch.int32, device="cuda")
+        got = binding.attn_decode(q, cache, table[:R, :wide], lens, scale=0.09, window=window, workspace=workspace)
+        check_decode(got, q, keys, 0.09, seen, window)
+        assert torch.equal(got, binding.attn_decode(q, cache, table[:R, :wide], lens, scale=0.09, window=window))
+
+
+@pytest.mark.gpu
+def test_steps_study_in_parts():
+    """A step of the study `steps` long enough for the shared launch, made twice: right, and the same bits."""
+    from paper_2601_16032_amd import sweeps
+    calls, held = sweeps.decode_step({"R": 3, "length": 4999, "H": 12, "KH": 4, "d": 128}, seed=3)
+    cache, outs = held["cache"], []
+    assert binding.attn_decode_workspace_bytes(3, 12, cache, held["table"].shape[1]) > 0
+    for _ in range(2):
+        for _, call in calls:
+            call()
+        outs.append(held["o"].clone())
+    keys = [[x[t.long()].transpose(1, 2).reshape(-1, 4, 128) for t in held["table"]] for x in (cache.k, cache.v)]
+    check_decode(outs[0], held["q"], keys, 128 ** -0.5, held["step"].lengths.tolist())
+    assert torch.equal(*outs) and held["step"].lengths.tolist() == [5000] * 3
