@@ -426,8 +426,9 @@ int attn_decode(const void* Q, int64_t q_request, int64_t q_head, void* O, int64
                 void* hip_stream);
 
 /* attn_decode_workspace_bytes -- the workspace attn_decode needs for R requests of H heads over `cache` (its pointers are not
- * looked at) with tables of max_pages entries: a function of these numbers alone, at most some tens of MiB.  The same workspace does for
- * every call of as many requests or fewer and tables as wide or narrower.  Launches nothing. */
+ * looked at) with tables of max_pages entries: a function of these numbers alone.  At most 17 MiB, or 64 d + 136 bytes for each query
+ * head to a key/value head where that is more (from 2140 on at d = 128).  The same workspace does for every call of as many requests or fewer and
+ * tables as wide or narrower.  Launches nothing. */
 int attn_decode_workspace_bytes(const sawattn_kv_cache* cache, int R, int H, int max_pages, size_t* bytes);
 
 /* Text of the last error raised on the calling thread ("" if none).  Static storage, never NULL. */

@@ -34,7 +34,7 @@ constexpr int kDecodeTile = 32;                                  // keys a wavef
 constexpr int kDecodeStep = kDecodeTile * kDecodeWaves;          // keys such a workgroup takes at a time: what is dealt out
 constexpr int kDecodeHeads = 16;                                 // query heads of a unit
 constexpr long long kDecodeDirectFew = 1 << 18, kDecodeDirectMany = 1 << 20;      // bytes of K and V of a unit at most, with fewer or more units than compute units
-constexpr int kDecodeGrid = 1024;                                // workgroups that share units: at most
+constexpr int kDecodeGrid = 1024;                                // workgroups that share units (half as many at d = 128), in all sets; eight a set at least
 constexpr int kDecodeUnits = 256;                                // compute units: up to as many workgroups of one step, then of two at least
 
 struct DecodeParams {

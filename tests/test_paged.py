@@ -1115,3 +1115,15 @@ def test_steps_study_in_parts():
     keys = [[x[t.long()].transpose(1, 2).reshape(-1, 4, 128) for t in held["table"]] for x in (cache.k, cache.v)]
     check_decode(outs[0], held["q"], keys, 128 ** -0.5, held["step"].lengths.tolist())
     assert torch.equal(*outs) and held["step"].lengths.tolist() == [5000] * 3
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_decode_workspace_stays_in_bounds(d):
+    """17 MiB, or 64 d + 136 bytes for each query head to a key head: long tables, whose need is largest, up to the most heads accepted."""
+    cache = cache_struct(d=d, heads=1)
+    sizes = {H: workspace_bytes(cache, 1, H, 16384) for H in [*range(1, 2100), 4111, 65536, 2 ** 20 + 16, 2 ** 22 - 1]}
+    for H, n in sizes.items():
+        assert n <= max(17 << 20, -(-H // 16) * 16 * (64 * d + 136)), (H, n)
+        assert H >= 2100 or n <= 17 << 20
+    assert max(n for H, n in sizes.items() if H <= 1024) > 10 << 20
+    assert workspace_bytes(cache_struct(d=d, heads=8), 511, 8 * 1024, 16384) <= 17 << 20
