@@ -128,6 +128,7 @@ def decode_step(pt, dtype="bf16", seed=0):
     new = torch.ones_like(lengths)
     workspace = torch.empty(sa.attn_decode_workspace_bytes(R, H, cache, held + 1), dtype=torch.uint8, device="cuda")
     step = sa.attn_kv_pages(lengths, new, table, free, state, page_size=ps, tokens=R)
+    q, k, v = qkv.split((H, KH, KH), 1)          # (2 us on the host, not of the call's)
     held_by = {"qkv": qkv, "cache": cache, "table": table, "step": step, "weight": weight, "frequencies": frequencies,
                "q": torch.empty(R, H, d, dtype=dt, device="cuda"), "o": torch.empty(R, H, d, dtype=dt, device="cuda")}
     return [
@@ -135,8 +136,8 @@ def decode_step(pt, dtype="bf16", seed=0):
             lengths, new, table, free, state, page_size=ps, lengths_out=step.lengths, granted=step.granted,
             token_offsets=step.token_offsets, free_state_out=step.free_state, slots=step.slots, positions=step.positions)),
         ("attn_qkv_prepare", lambda: sa.attn_qkv_prepare(
-            qkv[:, :H], qkv[:, H:H + KH], qkv[:, H + KH:], positions=step.positions, frequencies=frequencies, q_weight=weight,
-            k_weight=weight, q_out=held_by["q"], cache=cache, slots=step.slots)),
+            q, k, v, positions=step.positions, frequencies=frequencies, q_weight=weight, k_weight=weight, q_out=held_by["q"], cache=cache,
+            slots=step.slots)),
         ("attn_decode", lambda: sa.attn_decode(held_by["q"], cache, table, step.lengths, held_by["o"], scale=1.0 / math.sqrt(d),
                                                workspace=workspace)),
     ], held_by
