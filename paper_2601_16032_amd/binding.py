@@ -328,6 +328,8 @@ class KVCache:
             raise ValueError("k and v must share shape, dtype and device")
         if k.dtype not in _IN_DTYPE_CODE:
             raise ValueError("a cache must be float16 or bfloat16")
+        if max(k.shape) > 2 ** 31 - 1:
+            raise ValueError("a cache must have fewer than 2^31 pages, heads and rows per page")
         self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.get_device()
         self.pages, self.heads, self.page_size, self.d = k.shape
         self._struct = _CacheStruct(k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3], self.pages, self.page_size,

@@ -1127,3 +1127,12 @@ def test_decode_workspace_stays_in_bounds(d):
         assert H >= 2100 or n <= 17 << 20
     assert max(n for H, n in sizes.items() if H <= 1024) > 10 << 20
     assert workspace_bytes(cache_struct(d=d, heads=8), 511, 8 * 1024, 16384) <= 17 << 20
+
+
+@pytest.mark.gpu
+def test_cache_of_too_many_pages():
+    """Counts that pass 32 bits are refused, not cut off (2^32 + 10 pages would be 10)."""
+    for shape, wide in (((1, 1, 16, 64), (2 ** 32 + 10, 1, 16, 64)), ((1, 1, 16, 64), (1, 2 ** 32 + 1, 16, 64)), ((1, 1, 1, 64), (1, 1, 2 ** 32 + 16, 64))):
+        x = torch.empty(shape, dtype=torch.float16, device="cuda").expand(wide)
+        with pytest.raises(ValueError, match="fewer than 2"):
+            binding.KVCache(x, x)
