@@ -385,7 +385,8 @@ int attn_kv_pages(const int32_t* lengths, const int32_t* new_tokens, int R, int3
  *   B, N, H, KH        >= 1; B*N below 2^26, H + 2*KH at most 2^16
  *   d, dtype           64 or 128, SAWATTN_F16 or SAWATTN_BF16, of all rows and of the cache
  * Other overlaps of outputs with inputs or with each other are not allowed (and not looked for).  Angles are reduced in 64 bits, all
- * else is computed in 32 (squares of elements beyond 10^18 overflow) and rounded once.  One launch; no workspace.  Stream and errors as attn_fwd.
+ * else is computed in 32 and rounded once.  (Squares of elements beyond 10^18 overflow; where eps is 0 those of elements below 10^-19 lose bits, and a
+ * normalised head of zeros, or of so small elements that all squares are 0, is no number or infinite.)  One launch; no workspace.  Stream and errors as attn_fwd.
  */
 int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache* cache, const int64_t* slots, const int32_t* positions,
                      const float* q_weight, const float* k_weight, float eps, const double* frequencies, int rotated,

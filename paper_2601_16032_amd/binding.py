@@ -409,7 +409,8 @@ def attn_qkv_prepare(q, k, v, *, positions, frequencies=None, interleaved: bool 
                      eps: float = 1e-6, q_out=None, k_out=None, v_out=None, cache: KVCache = None, slots=None, stream=None):
     """Norms of the heads of Q and K (where a weight is given) and rotation of their first 2 * len(frequencies) elements, K and V
     written to `slots` of the cache and / or to k_out and v_out.  q, k, v: [B, N, heads, d] or [N, heads, d], of any strides.
-    Returns (q_out, k_out, v_out); q_out is made where it is not given, k_out and v_out where there is no cache either."""
+    Returns (q_out, k_out, v_out); q_out is made where it is not given, k_out and v_out where there is no cache either.  A token of negative
+    position is padding: its rows of the outputs are left as they are, in those made here whatever the memory held."""
     if (cache is None) != (slots is None) or (k_out is None) != (v_out is None):
         raise ValueError("cache and slots, and k_out and v_out, must be given together")
     if q_out is None:
