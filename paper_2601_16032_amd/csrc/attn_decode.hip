@@ -9,7 +9,7 @@
 // steps of 128, and the steps of all units, one behind the other, are dealt out evenly: workgroup w takes `share` of them from w * share on, whatever the
 // lengths are, so that one long request and many short ones load the chip alike and the host needs to know no length.  A workgroup ends at
 // most two units unfinished, its first and its last; of those it leaves (m, sum, O) of its part in one of its two places in the workspace,
-// and a second kernel joins them.  Measured (16 x 32768, ungrouped): 256, 512, 1024 and 2048 workgroups 660, 660, 670 and 690 us; ragged requests want
+// and a second kernel joins them.  Measured (here and below: calls captured into a graph, inputs changing; 16 x 32768, ungrouped): 256, 512, 1024 and 2048 workgroups 660, 660, 670 and 690 us; ragged requests want
 // two workgroups to a compute unit, so that one loads while the other ends a unit (64 requests up to 8192: 95 us, one of eight wavefronts 103).
 //
 // Within a workgroup every wavefront takes tiles of 32 keys of its own, with its own running maximum and sum; they are added up in LDS at the
@@ -62,7 +62,7 @@ struct DecodeParams {
 
 // Workgroups come in one set for each head group, which share their keys and values: the same workgroup of all sets on one XCD (blocks go
 // round the eight of them), one behind the other, so that what the first brings into the L2 the others find there (16 requests x 30000 keys, one
-// key head: 16 query heads 51 us, 64 99; read anew by every set 161).
+// key head: 16 query heads 52 us, 64 102; read anew by every set 161).
 __device__ __forceinline__ int block_of(const DecodeParams& p, int workgroup, int head_group) {
     return p.head_groups == 1 ? workgroup : (workgroup / 8 * p.head_groups + head_group) * 8 + workgroup % 8;
 }
@@ -448,8 +448,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void decode_kernel(DecodeParams p) {
 }
 
 // Adds up the parts of the units that several workgroups shared, a workgroup for every two heads of each, and clears the rows of empty
-// requests.  The threads that hold a head's elements, four each, go over every kGroups-th part, four parts on their way at a time.  It takes 4 us, of which
-// the parts are the least: launch, record of the unit, parts, result, one after the other.  (Two heads and 256 threads: 1 x 1000 keys 10.9 us in all, with
+// requests.  The threads that hold a head's elements, four each, go over every kGroups-th part, four parts on their way at a time.  It takes 4 us (6.5 where
+// a unit has 64 parts), of which the parts are the least: launch, record of the unit, parts, result, one after the other.  (Two heads and 256 threads: 1 x 1000 keys 10.9 us in all, with
 // four and 1024 11.2; parts fetched before the record is there: 0.3 to 1 us more.)
 constexpr int kJoinThreads = 256, kJoinHeads = 2, kJoinAhead = 4;
 
@@ -542,7 +542,7 @@ int decode_plan(const sawattn_kv_cache* cache, int R, int H, int max_pages, int 
     const double most = (double)R * out->units * ((capacity + kDecodeStep - 1) / kDecodeStep);      // steps
     if (most >= 2147483648.0 - 2.0 * kDecodeGrid)
         return fail(SAWATTN_ERR_INVALID_ARG, "R*heads*ceil(max_pages*page_size/128) must be below 2^31 - 2048");
-    // One workgroup reads about 55 GB/s, the second kernel costs 6 us and more.  Few units: up to 500 keys at d = 128 take 8.5 us in one launch,
+    // One workgroup reads about 55 GB/s, the second kernel costs 6 us and more with the 2 us in front of it.  Few units: up to 500 keys at d = 128 take 8.5 us in one launch,
     // in two 9; 1000 keys 12.5 and 9.4.  Units for every compute unit and more: 256 requests of 1000 keys, 8 heads: 170 and 190 us, 128 ragged
     // requests up to 2000: 57 and 62.
     const long long units = (long long)R * out->units, bytes = 4LL * out->seen * cache->d, sets = out->head_groups;

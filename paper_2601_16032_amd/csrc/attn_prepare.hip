@@ -8,7 +8,7 @@
 // lane, which then takes the four it turns its four pairs of elements by from other lanes.  With pairs (i, i + rotated/2) a lane holds
 // elements 4j.. and rotated/2 + 4j.., two pieces of 8 bytes, and no element changes lanes; with pairs (2i, 2i + 1) one piece of 16 bytes.
 // Rows are stored non-temporally (2048 tokens of 48 heads 22.8 -> 14.8 us) and loaded a trip ahead.  32 + 2 x 8 heads x 16384 into the cache, 403 MB:
-// 77 us, 5.2 TB/s (a copy of 2 GiB: 4.8).  Angles: position * frequency / 2 pi in 64 bits, less its nearest
+// 77 us, 5.2 TB/s (calls captured into a graph, inputs changing; the same bytes copied non-temporally 64 us, 6.3 TB/s).  Angles: position * frequency / 2 pi in 64 bits, less its nearest
 // whole number; in 32 bits it would be off by 0.06 of a radian at position 10^6.  Sums, norms and turns are in 32 bits, and there is one
 // rounding, to the type of the rows.
 namespace sawattn {
