@@ -417,7 +417,8 @@ int attn_qkv_prepare(const sawattn_qkv* rows, const sawattn_kv_cache* cache, con
  * A request of length 0 gets zeros.  A row of the cache outside the visible ones is never used, whatever it holds.  An infinity among the visible
  * values makes the elements it meets infinite (NaN where there is one of either sign), NaN if its probability is less than 2^-38 of the largest.
  * A table entry outside 0 .. pages - 1 among the visible ones makes the request's O NaN.  Products are exact, scores, probabilities, sums and O are held
- * in 32 bits (the probabilities enter the second product as sums of three 16-bit numbers).  The result does not depend on timing.
+ * in 32 bits (the probabilities enter the second product as sums of three 16-bit numbers; at binary16 they end at 2^-38 of the largest).  The result does
+ * not depend on timing.
  * One launch where the rows that can be visible are few (up to 256 KiB of K and V per request and key/value head, or 1 MiB with
  * 256 of those and more), else two.  Stream and errors as attn_fwd.
  */

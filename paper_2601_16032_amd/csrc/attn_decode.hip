@@ -129,16 +129,23 @@ struct DecodePieces {
     static constexpr int kCount = 3;
     unsigned word[kCount];
     __device__ __forceinline__ DecodePieces(float a, float b) {
-        constexpr float kLeast = BF16 ? 0x1p-100f : 0x1p-24f;
-        const float least_a = fminf(a, kLeast), least_b = fminf(b, kLeast);
+        if constexpr (BF16) {      // eight bits at a time, of the next smaller number, so that something is left
 #pragma unroll
-        for (int i = 0; i < kCount; ++i) {
-            if (i) {
-                a = fmaxf(a - widen<BF16>(word[i - 1], 0), least_a);
-                b = fmaxf(b - widen<BF16>(word[i - 1], 1), least_b);
+            for (int i = 0; i < kCount; ++i) {
+                const unsigned one = i + 1 < kCount ? 1u : 0u;
+                const unsigned x = __builtin_elementwise_sub_sat(__builtin_bit_cast(unsigned, a), one), y = __builtin_elementwise_sub_sat(__builtin_bit_cast(unsigned, b), one);
+                word[i] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+                a -= __builtin_bit_cast(float, x & 0xffff0000u);
+                b -= __builtin_bit_cast(float, y & 0xffff0000u);
             }
-            if constexpr (BF16) word[i] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
-            else word[i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(a, b));
+        } else {      // eleven bits; what is left is at least the smallest number there is, where the probability is
+            const float least_a = fminf(a, 0x1p-24f), least_b = fminf(b, 0x1p-24f);
+#pragma unroll
+            for (int i = 0; i < kCount; ++i) {
+                word[i] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(a, b));
+                a = fmaxf(a - widen<false>(word[i], 0), least_a);
+                b = fmaxf(b - widen<false>(word[i], 1), least_b);
+            }
         }
     }
 };

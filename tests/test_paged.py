@@ -1136,3 +1136,18 @@ def test_cache_of_too_many_pages():
         x = torch.empty(shape, dtype=torch.float16, device="cuda").expand(wide)
         with pytest.raises(ValueError, match="fewer than 2"):
             binding.KVCache(x, x)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,wide", [(64, 1), (128, 400)])
+def test_decode_large_values_of_tiny_weight(d, wide):
+    """Values of 2^127 with probabilities of e^-60 to e^-80: what a probability holds does not end with the largest one's last bit.  The operand of exp2 is
+    116 at most and rounded twice (2^-24 each: 2^-16.6 of the probability), and at e^-80 the third number is subnormal (2^-16)."""
+    R = 300
+    q, cache, table, _ = weighed(R, d, "bf16", wide)
+    x = torch.linspace(60, 80, R, device="cuda").bfloat16()
+    cache.k[:, 0, 1, 3] = -x
+    cache.v[:, 0, 1] = 2.0 ** 127
+    got = f64(binding.attn_decode(q, cache, table, torch.full((R,), 2, dtype=torch.int32, device="cuda"), scale=1.0, o_dtype=torch.float32))
+    want = np.exp(-f64(x))[:, None, None] * 2.0 ** 127
+    assert (np.abs(got - want) <= 2.0 ** -15 * want).all(), float((np.abs(got - want) / want).max())
