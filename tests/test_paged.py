@@ -918,7 +918,8 @@ def weighed(R, d, dtype, wide):
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_decode_probabilities_in_32_bits(dtype, d, wide):
     """Off by 2^-20 at most, relative: the operand of exp2 is 2.9 at most and rounded twice (constant and product, 2^-24 each: 2^-22 of the
-    probability), exp2 one unit in the last place (2^-23), the second product three additions (2^-23 each), the sum and the quotient one unit.
+    probability), exp2 one unit in the last place (2^-23), the second product three additions (2^-23 each), the sum and the quotient one unit and a
+    half: 7.5 x 2^-23.  Binary16 adds 15 to the operand, which is rounded to 2^-21 then (2^-21.5 of the probability): 10.4 x 2^-23.
     Probabilities in 16 bits are off by 2^-17."""
     R = 384
     q, cache, table, p = weighed(R, d, dtype, wide)
@@ -926,7 +927,7 @@ def test_decode_probabilities_in_32_bits(dtype, d, wide):
     got = f64(binding.attn_decode(q, cache, table, torch.full((R,), 2, dtype=torch.int32, device="cuda"), scale=1.0, o_dtype=torch.float32))
     want = (p / (1 + p))[:, None, None]
     off = np.abs(got - want) / want
-    assert off.max() <= 2.0 ** -20, math.log2(off.max())
+    assert off.max() <= (1.5 if dtype == "f16" else 1) * 2.0 ** -20, math.log2(off.max())
 
 
 @pytest.mark.gpu
