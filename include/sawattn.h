@@ -433,6 +433,96 @@ int attn_decode(const void* Q, int64_t q_request, int64_t q_head, void* O, int64
  * tables as wide or narrower.  Launches nothing. */
 int attn_decode_workspace_bytes(const sawattn_kv_cache* cache, int R, int H, int max_pages, size_t* bytes);
 
+/*
+ * Requests that share pages.  Beams, several answers to a prompt and prompts kept for later requests have rows in common, which several rows of
+ * the table may then name the pages of: attn_kv_fork makes such tables and gives back pages that nobody holds any more, attn_kv_copy copies
+ * the part-filled pages that cannot be shared, attn_kv_shared_rows finds what a group of requests has in common, and attn_decode_shared
+ * reads that once for all of the group.  attn_kv_pages, attn_qkv_prepare and attn_decode work on shared pages as they are, with one exception: a
+ * request that may share pages is not ended by SAWATTN_REQUEST_ENDS (which gives back all of its pages) but by attn_kv_fork.
+ */
+
+/*
+ * attn_kv_fork -- the requests of the next step out of those of the last: go on, branch, change places, be cut short, end.
+ * Request r of the new batch takes over the first n = min(lengths[s], rows[r]) rows of request s = source[r] of the old one.  The pages that these rows fill are
+ * shared; a part-filled last page has one holder:
+ *   - where it is the source's own part-filled last page, the first request (lowest r) that ends in it takes it over;
+ *   - every other one takes a fresh page from the front of the free list, in the order of the requests, and copies[r] says what has to be copied
+ *     into it.  Where no page is left the request gets nothing: its length becomes 0 and copies[r] = (page, -1, rows).
+ * Every page that a request of the old batch holds and none of the new one does goes behind the last free one, in the order of their numbers (to be
+ * taken from the next call on).  A request of the old batch that no new one names has ended.
+ *
+ *   lengths         device, read: int32 [R], 1 <= R <= SAWATTN_MOST_REQUESTS.  Below 0 they count as 0, above max_pages*page_size as that.
+ *   source          device, read: int32 [N], 1 <= N <= SAWATTN_MOST_REQUESTS; outside 0 .. R - 1: an empty request
+ *   rows            device, read: int32 [N], or NULL: all rows.  Negative ones count as 0.
+ *   table           device, read: int32 [R] rows of max_pages >= 1 entries, table_stride apart.  Pages outside 0 .. pages - 1 are handed on but never given back.
+ *                   A part-filled last page must not be in another row (attn_kv_pages and this call see to that).
+ *   table_out       device, written: int32 [N] rows, likewise; entries behind a request's pages are left as they are
+ *   max_pages, page_size  as in attn_kv_pages (R*max_pages and N*max_pages below 2^31)
+ *   pages           of the cache, >= 1
+ *   free_pages      device, read and written: int32 [ring], as in attn_kv_pages
+ *   free_state      device, read: int32 [2]
+ *   lengths_out     device, written: int32 [N]
+ *   copies          device, written: int32 [N][3] = (page to copy from, page to copy to, rows), (-1, -1, 0) where there is nothing to copy
+ *   free_state_out  device, written: int32 [2]
+ *   workspace       device, written, 16-byte aligned, of at least attn_kv_fork_workspace_bytes; nothing in it has to start out zero
+ * Outputs may overlap neither each other nor the inputs.  The result does not depend on timing.  Up to three launches.  Stream and errors as attn_fwd.
+ */
+int attn_kv_fork(const int32_t* lengths, int R, const int32_t* source, const int32_t* rows, int N, const int32_t* table, int64_t table_stride,
+                 int32_t* table_out, int64_t table_out_stride, int max_pages, int page_size, int pages, int32_t* free_pages, int ring,
+                 const int32_t* free_state, int32_t* lengths_out, int32_t* copies, int32_t* free_state_out, void* workspace,
+                 size_t workspace_bytes, void* hip_stream);
+
+/* attn_kv_fork_workspace_bytes -- the workspace attn_kv_fork needs: 2 bytes a page, 8 a new request and some; enough for fewer of each too. */
+int attn_kv_fork_workspace_bytes(int R, int N, int pages, size_t* bytes);
+
+/*
+ * attn_kv_copy -- copies the first copies[i][2] rows of page copies[i][0] to page copies[i][1], K and V, all heads, in every one of the caches.
+ *
+ *   caches   host array of `layers` >= 1 structs, read during the call; alike in all but pointers and strides
+ *   copies   device, read: int32 [n][3], 1 <= n <= SAWATTN_MOST_REQUESTS, n*heads*page_size below 2^31.  An entry with a page outside
+ *            0 .. pages - 1, or twice the same one, copies nothing; rows count as 0 .. page_size.
+ * No page may be written twice, or written and read (the list of attn_kv_fork has no such ones).  One launch for 32 caches; no workspace.  Stream and
+ * errors as attn_fwd.
+ */
+int attn_kv_copy(const sawattn_kv_cache* caches, int layers, const int32_t* copies, int n, void* hip_stream);
+
+/*
+ * attn_kv_shared_rows -- how many leading rows the requests of a group have in the same pages, in whole pages that all of them have filled.
+ * Group g is the requests group_offsets[g] .. group_offsets[g + 1] - 1.  Requests of length 0 and below are left out; without any other the answer is 0.
+ *
+ *   lengths        device, read: int32 [R], 1 <= R <= SAWATTN_MOST_REQUESTS
+ *   table          device, read: int32 [R] rows of max_pages >= 1 entries, table_stride apart; max_pages*page_size below 2^31
+ *   group_offsets  device, read: int32 [groups + 1], 1 <= groups <= SAWATTN_MOST_REQUESTS; outside 0 .. R they count as the nearest of these
+ *   shared         device, written: int32 [groups], must not overlap the inputs
+ * One launch; no workspace.  Stream and errors as attn_fwd.
+ */
+int attn_kv_shared_rows(const int32_t* lengths, int R, const int32_t* table, int64_t table_stride, int max_pages, int page_size,
+                        const int32_t* group_offsets, int groups, int32_t* shared, void* hip_stream);
+
+/*
+ * attn_decode_shared -- attn_decode for requests in groups that begin with the same rows, which are read once for a group.  Group g is the requests
+ * group_offsets[g] .. group_offsets[g + 1] - 1.  Its requests have their first shared[g] rows in common, or as many of them as the shortest one
+ * holds that is not empty, in whole pages; these are read where the table says so for the first request that is not empty, all others, and those
+ * of requests in no group, where it says so for the request itself.
+ *
+ *   Q .. scale      as in attn_decode.  R at most SAWATTN_MOST_REQUESTS, R*H*ceil(max_pages*page_size/128) below 2^31 - 2048.
+ *   group_offsets   device, read: int32 [groups + 1], 1 <= groups <= SAWATTN_MOST_REQUESTS; outside 0 .. R they count as the nearest of these.
+ *                   They must not fall; if they do, nothing is taken to be shared.
+ *   shared          device, read: int32 [groups]; what attn_kv_shared_rows finds, or less
+ *   workspace       device, written, 16-byte aligned, of at least attn_decode_shared_workspace_bytes; used by this call's kernels only
+ * The result is that of attn_decode where the tables do name the same pages (or pages that hold the same), up to rounding: of the probabilities of shared rows 16 bits (bfloat16) or
+ * 22 (binary16, ending at 2^-39 of the largest) enter the second product.  Requests of length 0, values that are infinite and pages that there are not as in
+ * attn_decode (a bad page among the shared ones makes O of the whole group NaN).  The result does not depend on timing.  Two launches.  Stream and errors as attn_fwd.
+ */
+int attn_decode_shared(const void* Q, int64_t q_request, int64_t q_head, void* O, int64_t o_request, int64_t o_head, int o_dtype,
+                       const sawattn_kv_cache* cache, const int32_t* table, int64_t table_stride, int max_pages, const int32_t* lengths,
+                       const int32_t* group_offsets, const int32_t* shared, int groups, int R, int H, float scale, void* workspace,
+                       size_t workspace_bytes, void* hip_stream);
+
+/* attn_decode_shared_workspace_bytes -- the workspace attn_decode_shared needs for R requests of H heads in `groups` groups: 2 d R H floats and at most some
+ * 44 MiB.  The same workspace does for every call of as many requests and groups or fewer.  Launches nothing. */
+int attn_decode_shared_workspace_bytes(const sawattn_kv_cache* cache, int R, int H, int groups, int max_pages, size_t* bytes);
+
 /* Text of the last error raised on the calling thread ("" if none).  Static storage, never NULL. */
 const char* attn_last_error(void);
 

@@ -106,6 +106,18 @@ def lib() -> ctypes.CDLL:
                                   ctypes.c_size_t, vp]
         L.attn_decode_workspace_bytes.restype = ci
         L.attn_decode_workspace_bytes.argtypes = [vp, ci, ci, ci, ctypes.POINTER(ctypes.c_size_t)]
+        L.attn_kv_fork.restype = ci
+        L.attn_kv_fork.argtypes = [vp, ci, vp, vp, ci, vp, i64, vp, i64, ci, ci, ci, vp, ci, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.attn_kv_fork_workspace_bytes.restype = ci
+        L.attn_kv_fork_workspace_bytes.argtypes = [ci, ci, ci, ctypes.POINTER(ctypes.c_size_t)]
+        L.attn_kv_copy.restype = ci
+        L.attn_kv_copy.argtypes = [vp, ci, vp, ci, vp]
+        L.attn_kv_shared_rows.restype = ci
+        L.attn_kv_shared_rows.argtypes = [vp, ci, vp, i64, ci, ci, vp, ci, vp, vp]
+        L.attn_decode_shared.restype = ci
+        L.attn_decode_shared.argtypes = [vp, i64, i64, vp, i64, i64, ci, vp, vp, i64, ci, vp, vp, vp, ci, ci, ci, ctypes.c_float, vp, ctypes.c_size_t, vp]
+        L.attn_decode_shared_workspace_bytes.restype = ci
+        L.attn_decode_shared_workspace_bytes.argtypes = [vp, ci, ci, ci, ci, ctypes.POINTER(ctypes.c_size_t)]
         for name in ("attn_last_error", "sawattn_last_error"):
             getattr(L, name).restype = ctypes.c_char_p
             getattr(L, name).argtypes = []
@@ -341,7 +353,7 @@ _paged = None
 
 
 def _paged_module():
-    """The module that looks at tensors and calls the library for the three operators below (built with the library), bound to it."""
+    """The module that looks at tensors and calls the library for the operators below (built with the library), bound to it."""
     global _paged
     if _paged is None:
         if not os.path.exists(PAGED_BINDING_PATH):
@@ -349,7 +361,8 @@ def _paged_module():
         L = lib()
         from . import _paged as module
         module.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-            L.attn_kv_pages, L.attn_qkv_prepare, L.attn_decode, L.hipGetDevice, L.hipSetDevice)))      # (the last two of the HIP runtime it loads)
+            L.attn_kv_pages, L.attn_qkv_prepare, L.attn_decode, L.hipGetDevice, L.hipSetDevice,      # (these two of the HIP runtime it loads)
+            L.attn_kv_fork, L.attn_kv_copy, L.attn_kv_shared_rows, L.attn_decode_shared)))
         _paged = module
     return _paged
 
@@ -446,6 +459,100 @@ def attn_decode(Q, cache: KVCache, table, lengths, O=None, *, scale: float, wind
         workspace = _empty(attn_decode_workspace_bytes(Q.shape[0], Q.shape[1], cache, table.shape[-1]), torch.uint8, Q.device, stream)
     device = cache.device
     rc = (_paged or _paged_module()).decode(Q, O, cache.ptr, device, table, lengths, scale, window, workspace, _stream_on(device, stream))
+    if rc != OK:
+        _check(rc)
+    return O
+
+
+# ---- requests that share pages
+
+class KVLayers:
+    """The caches of several layers, alike in all but strides (and places), for calls that work on all of them.  Made once, kept with the caches."""
+
+    def __init__(self, caches):
+        self.caches = tuple(caches)
+        if not self.caches:
+            raise ValueError("there must be a cache")
+        one = self.caches[0]
+        for c in self.caches:
+            if (c.pages, c.heads, c.page_size, c.d, c.dtype, c.device) != (one.pages, one.heads, one.page_size, one.d, one.dtype, one.device):
+                raise ValueError("the caches must share shape, dtype and device")
+        self.count, self.device = len(self.caches), one.device
+        self._structs = (_CacheStruct * self.count)(*(c._struct for c in self.caches))
+        self.ptr = ctypes.addressof(self._structs)
+
+
+class ForkStep(NamedTuple):
+    """What attn_kv_fork writes."""
+    table: torch.Tensor           # int32 [N, pages]
+    lengths: torch.Tensor         # int32 [N]
+    copies: torch.Tensor          # int32 [N, 3]
+    free_state: torch.Tensor      # int32 [2]
+
+
+def attn_kv_fork_workspace_bytes(R: int, N: int, pages: int) -> int:
+    """Bytes of workspace attn_kv_fork needs for R requests that become N, or fewer, over a cache of that many pages, or fewer."""
+    n = ctypes.c_size_t(0)
+    _check(lib().attn_kv_fork_workspace_bytes(R, N, pages, ctypes.byref(n)))
+    return int(n.value)
+
+
+def attn_kv_fork(lengths, source, table, free_pages, free_state, *, page_size: int, pages: int, rows=None, table_out=None, lengths_out=None, copies=None,
+                 free_state_out=None, workspace=None, stream=None) -> ForkStep:
+    """The requests of the next step: request r goes on from the first rows[r] (None: all) rows of request source[r], or is empty (-1).  Whole pages are
+    shared, `copies` says which part-filled ones are to be copied (attn_kv_copy), pages that nobody holds any more go back to the ring `free_pages`, in place.  The
+    rest is written to the tensors given or to new ones; entries of table_out behind a request's pages are left as they are, in one made here whatever
+    the memory held.  workspace: a uint8 tensor of at least attn_kv_fork_workspace_bytes bytes, made here when None."""
+    device, N = lengths.device, source.numel()
+    if table_out is None:
+        table_out = _empty((N, table.shape[-1]), torch.int32, device, stream)
+    if lengths_out is None or copies is None or free_state_out is None:
+        lengths_out, copies, free_state_out = (_empty(size, torch.int32, device, stream) if t is None else t
+                                               for t, size in ((lengths_out, N), (copies, (N, 3)), (free_state_out, 2)))
+    if workspace is None:
+        workspace = _empty(attn_kv_fork_workspace_bytes(lengths.numel(), N, pages), torch.uint8, device, stream)
+    rc = (_paged or _paged_module()).kv_fork(lengths, source, rows, table, table_out, free_pages, free_state, lengths_out, copies, free_state_out, workspace,
+                                             page_size, pages, _stream_on(lengths.get_device(), stream))
+    if rc != OK:
+        _check(rc)
+    return ForkStep(table_out, lengths_out, copies, free_state_out)
+
+
+def attn_kv_copy(caches, copies, stream=None):
+    """Copies rows of pages as copies[i] = (from, to, rows) says, K and V, all heads, in a KVCache or in all caches of a KVLayers.  Returns without waiting."""
+    layers = caches.count if isinstance(caches, KVLayers) else 1
+    device = caches.device
+    rc = (_paged or _paged_module()).kv_copy(caches.ptr, layers, device, copies, _stream_on(device, stream))
+    if rc != OK:
+        _check(rc)
+
+
+def attn_kv_shared_rows(table, lengths, group_offsets, *, page_size: int, shared=None, stream=None):
+    """How many leading rows the requests group_offsets[g] .. group_offsets[g + 1] - 1 have in the same pages, for every g: int32 [groups]."""
+    if shared is None:
+        shared = _empty(group_offsets.numel() - 1, torch.int32, lengths.device, stream)
+    rc = (_paged or _paged_module()).kv_shared_rows(lengths, table, group_offsets, shared, page_size, _stream_on(lengths.get_device(), stream))
+    if rc != OK:
+        _check(rc)
+    return shared
+
+
+def attn_decode_shared_workspace_bytes(R: int, H: int, groups: int, cache: KVCache, max_pages: int) -> int:
+    """Bytes of workspace attn_decode_shared needs for R requests of H heads in that many groups, or fewer, and page tables of max_pages entries."""
+    n = ctypes.c_size_t(0)
+    _check(lib().attn_decode_shared_workspace_bytes(cache.ptr, R, H, groups, max_pages, ctypes.byref(n)))
+    return int(n.value)
+
+
+def attn_decode_shared(Q, cache: KVCache, table, lengths, group_offsets, shared, O=None, *, scale: float, o_dtype=None, workspace=None, stream=None):
+    """attn_decode for requests in groups: the first shared[g] rows of the requests group_offsets[g] .. group_offsets[g + 1] - 1 are read once, by the table row
+    of the first of them.  workspace: a uint8 tensor of at least attn_decode_shared_workspace_bytes bytes, made here when None.  Returns O without waiting."""
+    if O is None:
+        O = _empty(Q.shape, o_dtype or Q.dtype, Q.device, stream)
+    if workspace is None:
+        workspace = _empty(attn_decode_shared_workspace_bytes(Q.shape[0], Q.shape[1], shared.numel(), cache, table.shape[-1]), torch.uint8, Q.device, stream)
+    device = cache.device
+    rc = (_paged or _paged_module()).decode_shared(Q, O, cache.ptr, device, table, lengths, group_offsets, shared, scale, workspace, _stream_on(device, stream))
     if rc != OK:
         _check(rc)
     return O

@@ -56,7 +56,7 @@ def check_wide_kernels(resources: dict) -> None:
 def check_scratch(resources: dict) -> None:
     """No attention kernel uses scratch memory: what spills is stored and loaded per query tile at best, a tenth of a short launch's time.
     Refuse a build in which one does, or in which there is nothing to look at."""
-    kernels = {k: v for k, v in resources.items() if "attn_fwd_" in k or re.search(r"\d(?:kv_pages|qkv_prepare|decode|decode_join)_kernel", k)}
+    kernels = {k: v for k, v in resources.items() if "attn_fwd_" in k or re.search(r"\d(?:kv_\w+?|qkv_prepare|decode\w*?)_kernel", k)}
     bad = {k: v.get("ScratchSize", -1) for k, v in kernels.items() if v.get("ScratchSize", -1) != 0}
     if bad or not kernels:
         raise RuntimeError(f"attention kernels must not use scratch memory (bytes per lane): {bad or 'no kernels found'}")

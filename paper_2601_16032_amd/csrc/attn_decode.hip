@@ -583,6 +583,54 @@ int launch_decode(const DecodeParams& p, const DecodePlan& plan, int H, hipStrea
 
 size_t decode_bytes(const DecodePlan& plan, int d) { return plan.direct ? 0 : (size_t)plan.grid * (2 * plan.heads_kept * (d + 2) * sizeof(float) + sizeof(int4)); }
 
+// Checks the arguments of attn_decode (those that decode_plan and check_cache leave) and fills in what the kernels get of them, the workspace apart.
+int decode_params(const void* Q, int64_t q_request, int64_t q_head, void* O, int64_t o_request, int64_t o_head, int o_dtype, const sawattn_kv_cache* cache,
+                  const int32_t* table, int64_t table_stride, int max_pages, const int32_t* lengths, int R, int H, float scale, int window, void* workspace,
+                  size_t workspace_bytes, size_t need, const DecodePlan& plan, DecodeParams* out) {
+    if (!Q || !O || !table || !lengths || (need && !workspace))
+        return fail(SAWATTN_ERR_INVALID_ARG, "Q, O, table, lengths and workspace must be non-null");
+    if (cache->k_row > (1 << 26) || cache->v_row > (1 << 26)) return fail(SAWATTN_ERR_UNSUPPORTED, "cache: row strides must be at most 2^26");
+    if (((uintptr_t)Q | (uintptr_t)O | (uintptr_t)workspace) & 15u)
+        return fail(SAWATTN_ERR_INVALID_ARG, "Q, O and workspace must be 16-byte aligned");
+    if (((uintptr_t)table | (uintptr_t)lengths) & 3u) return fail(SAWATTN_ERR_INVALID_ARG, "table and lengths must be 4-byte aligned");
+    if (o_dtype != SAWATTN_F16 && o_dtype != SAWATTN_BF16 && o_dtype != SAWATTN_F32)
+        return fail(SAWATTN_ERR_INVALID_ARG, "o_dtype must be SAWATTN_F16, SAWATTN_BF16 or SAWATTN_F32");
+    if (!std::isfinite(scale)) return fail(SAWATTN_ERR_INVALID_ARG, "scale must be finite");
+    if (table_stride < max_pages || (double)table_stride * R >= 1e18)
+        return fail(SAWATTN_ERR_INVALID_ARG, "table_stride must be at least max_pages");
+    const int d = cache->d;
+    if (!good_stride(q_request, R) || !good_stride(q_head, H) || !good_stride(o_request, R) || !good_stride(o_head, H))
+        return fail(SAWATTN_ERR_INVALID_ARG, "strides of Q and O must be multiples of 8, not negative");
+    if ((R > 1 && o_request < d) || (H > 1 && o_head < d)) return fail(SAWATTN_ERR_INVALID_ARG, "strides of O must be at least d");
+    if (workspace_bytes < need)
+        return fail(SAWATTN_ERR_INVALID_ARG, "workspace is smaller than attn_decode_workspace_bytes reports");
+    const int o_size = o_dtype == SAWATTN_F32 ? 4 : 2;
+    auto extent = [](int n, int64_t stride) { return n > 1 ? (unsigned long long)(n - 1) * stride : 0ull; };
+    const Range o(O, o_size * (extent(R, o_request) + extent(H, o_head) + d));
+    const Range scratch(workspace, need);
+    const Range in[] = {
+        {Q, 2 * (extent(R, q_request) + extent(H, q_head) + d)},
+        {cache->k, 2 * (extent(cache->pages, cache->k_page) + extent(cache->heads, cache->k_head) + extent(cache->page_size, cache->k_row) + d)},
+        {cache->v, 2 * (extent(cache->pages, cache->v_page) + extent(cache->heads, cache->v_head) + extent(cache->page_size, cache->v_row) + d)},
+        {table, 4 * (extent(R, table_stride) + max_pages)}, {lengths, 4ull * R}};
+    for (const Range& i : in)
+        if (o.meets(i) || scratch.meets(i)) return fail(SAWATTN_ERR_INVALID_ARG, "O and workspace must not overlap what is read");
+    if (o.meets(scratch)) return fail(SAWATTN_ERR_INVALID_ARG, "O must not overlap the workspace");
+
+    *out = DecodeParams{};
+    DecodeParams& p = *out;
+    p.Q = static_cast<const char*>(Q); p.q_request = 2 * q_request; p.q_head = 2 * q_head;
+    p.O = static_cast<char*>(O); p.o_request = o_size * o_request; p.o_head = o_size * o_head; p.o_dtype = o_dtype;
+    p.K = static_cast<const char*>(cache->k); p.V = static_cast<const char*>(cache->v);
+    p.k_page = 2 * cache->k_page; p.k_head = 2 * cache->k_head; p.k_row = (unsigned)(2 * cache->k_row);
+    p.v_page = 2 * cache->v_page; p.v_head = 2 * cache->v_head; p.v_row = (unsigned)(2 * cache->v_row);
+    p.table = table; p.table_stride = table_stride; p.lengths = lengths;
+    p.c = (float)((double)scale * 1.4426950408889634074);
+    p.R = R; p.capacity = max_pages * cache->page_size; p.window = window; p.pages = cache->pages; p.shift = page_shift(cache->page_size);
+    p.group = plan.group; p.head_groups = plan.head_groups; p.units = plan.units; p.workgroups = plan.workgroups; p.heads_kept = plan.heads_kept;
+    return SAWATTN_OK;
+}
+
 }  // namespace sawattn
 
 extern "C" {
@@ -618,51 +666,16 @@ int attn_decode(const void* Q, int64_t q_request, int64_t q_head, void* O, int64
     rc = decode_plan(cache, R, H, max_pages, window, &plan);
     if (rc != SAWATTN_OK) return rc;
     const size_t need = decode_bytes(plan, cache->d);
-    if (!Q || !O || !table || !lengths || (need && !workspace))
-        return fail(SAWATTN_ERR_INVALID_ARG, "Q, O, table, lengths and workspace must be non-null");
-    if (cache->k_row > (1 << 26) || cache->v_row > (1 << 26)) return fail(SAWATTN_ERR_UNSUPPORTED, "cache: row strides must be at most 2^26");
-    if (((uintptr_t)Q | (uintptr_t)O | (uintptr_t)workspace) & 15u)
-        return fail(SAWATTN_ERR_INVALID_ARG, "Q, O and workspace must be 16-byte aligned");
-    if (((uintptr_t)table | (uintptr_t)lengths) & 3u) return fail(SAWATTN_ERR_INVALID_ARG, "table and lengths must be 4-byte aligned");
-    if (o_dtype != SAWATTN_F16 && o_dtype != SAWATTN_BF16 && o_dtype != SAWATTN_F32)
-        return fail(SAWATTN_ERR_INVALID_ARG, "o_dtype must be SAWATTN_F16, SAWATTN_BF16 or SAWATTN_F32");
-    if (!std::isfinite(scale)) return fail(SAWATTN_ERR_INVALID_ARG, "scale must be finite");
-    if (table_stride < max_pages || (double)table_stride * R >= 1e18)
-        return fail(SAWATTN_ERR_INVALID_ARG, "table_stride must be at least max_pages");
+    DecodeParams p;
+    rc = decode_params(Q, q_request, q_head, O, o_request, o_head, o_dtype, cache, table, table_stride, max_pages, lengths, R, H, scale, window, workspace,
+                       workspace_bytes, need, plan, &p);
+    if (rc != SAWATTN_OK) return rc;
     const int d = cache->d;
-    if (!good_stride(q_request, R) || !good_stride(q_head, H) || !good_stride(o_request, R) || !good_stride(o_head, H))
-        return fail(SAWATTN_ERR_INVALID_ARG, "strides of Q and O must be multiples of 8, not negative");
-    if ((R > 1 && o_request < d) || (H > 1 && o_head < d)) return fail(SAWATTN_ERR_INVALID_ARG, "strides of O must be at least d");
-    if (workspace_bytes < need)
-        return fail(SAWATTN_ERR_INVALID_ARG, "workspace is smaller than attn_decode_workspace_bytes reports");
-    const int o_size = o_dtype == SAWATTN_F32 ? 4 : 2;
-    auto extent = [](int n, int64_t stride) { return n > 1 ? (unsigned long long)(n - 1) * stride : 0ull; };
-    const Range o(O, o_size * (extent(R, o_request) + extent(H, o_head) + d));
-    const Range scratch(workspace, need);
-    const Range in[] = {
-        {Q, 2 * (extent(R, q_request) + extent(H, q_head) + d)},
-        {cache->k, 2 * (extent(cache->pages, cache->k_page) + extent(cache->heads, cache->k_head) + extent(cache->page_size, cache->k_row) + d)},
-        {cache->v, 2 * (extent(cache->pages, cache->v_page) + extent(cache->heads, cache->v_head) + extent(cache->page_size, cache->v_row) + d)},
-        {table, 4 * (extent(R, table_stride) + max_pages)}, {lengths, 4ull * R}};
-    for (const Range& i : in)
-        if (o.meets(i) || scratch.meets(i)) return fail(SAWATTN_ERR_INVALID_ARG, "O and workspace must not overlap what is read");
-    if (o.meets(scratch)) return fail(SAWATTN_ERR_INVALID_ARG, "O must not overlap the workspace");
-
-    DecodeParams p{};
-    p.Q = static_cast<const char*>(Q); p.q_request = 2 * q_request; p.q_head = 2 * q_head;
-    p.O = static_cast<char*>(O); p.o_request = o_size * o_request; p.o_head = o_size * o_head; p.o_dtype = o_dtype;
-    p.K = static_cast<const char*>(cache->k); p.V = static_cast<const char*>(cache->v);
-    p.k_page = 2 * cache->k_page; p.k_head = 2 * cache->k_head; p.k_row = (unsigned)(2 * cache->k_row);
-    p.v_page = 2 * cache->v_page; p.v_head = 2 * cache->v_head; p.v_row = (unsigned)(2 * cache->v_row);
-    p.table = table; p.table_stride = table_stride; p.lengths = lengths;
     if (need) {
         p.parts = static_cast<float*>(workspace);
         p.begun = reinterpret_cast<int4*>(p.parts + (size_t)2 * plan.grid * plan.heads_kept * d);
         p.part_sums = reinterpret_cast<f2*>(p.begun + plan.grid);
     }
-    p.c = (float)((double)scale * 1.4426950408889634074);
-    p.R = R; p.capacity = max_pages * cache->page_size; p.window = window; p.pages = cache->pages; p.shift = page_shift(cache->page_size);
-    p.group = plan.group; p.head_groups = plan.head_groups; p.units = plan.units; p.workgroups = plan.workgroups; p.heads_kept = plan.heads_kept;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const bool bf = cache->dtype == SAWATTN_BF16;
     if (d == 128) return bf ? launch_decode<128, true>(p, plan, H, stream) : launch_decode<128, false>(p, plan, H, stream);

@@ -2,7 +2,7 @@
 // handing their addresses to the library.  A decoding step makes these calls once per layer, and in Python the look alone took as long as
 // the launch (attn_kv_pages 3.7 of 7.8 us, attn_qkv_prepare 4.4 of 8.5); here, with the launch, a call takes 4 us.
 //
-// A Python module of three functions that take everything by position and return the library's code; a tensor that does not fit is a ValueError.  The
+// A Python module of functions that take everything by position and return the library's code; a tensor that does not fit is a ValueError.  The
 // library's functions are handed in (bind), so that there is one copy of it in the process, whoever loaded it.
 #include <Python.h>
 
@@ -18,6 +18,10 @@ namespace {
 decltype(&attn_kv_pages) g_kv_pages;
 decltype(&attn_qkv_prepare) g_qkv_prepare;
 decltype(&attn_decode) g_decode;
+decltype(&attn_kv_fork) g_kv_fork;
+decltype(&attn_kv_copy) g_kv_copy;
+decltype(&attn_kv_shared_rows) g_kv_shared_rows;
+decltype(&attn_decode_shared) g_decode_shared;
 int (*g_get_device)(int*);      // hipGetDevice, hipSetDevice
 int (*g_set_device)(int);
 
@@ -122,14 +126,16 @@ PyObject* guarded(Py_ssize_t given, Py_ssize_t wanted, F&& f) {
     }
 }
 
-// bind(addresses of attn_kv_pages, attn_qkv_prepare, attn_decode, hipGetDevice, hipSetDevice)
+// bind(addresses of attn_kv_pages, attn_qkv_prepare, attn_decode, hipGetDevice, hipSetDevice, attn_kv_fork, attn_kv_copy, attn_kv_shared_rows,
+//      attn_decode_shared)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 5) {
-        PyErr_SetString(PyExc_TypeError, "five addresses expected");
+    constexpr int kAddresses = 9;
+    if (n != kAddresses) {
+        PyErr_SetString(PyExc_TypeError, "nine addresses expected");
         return nullptr;
     }
-    void* p[5];
-    for (int i = 0; i < 5; ++i) {
+    void* p[kAddresses];
+    for (int i = 0; i < kAddresses; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a null address");
@@ -141,6 +147,10 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g_decode = reinterpret_cast<decltype(g_decode)>(p[2]);
     g_get_device = reinterpret_cast<decltype(g_get_device)>(p[3]);
     g_set_device = reinterpret_cast<decltype(g_set_device)>(p[4]);
+    g_kv_fork = reinterpret_cast<decltype(g_kv_fork)>(p[5]);
+    g_kv_copy = reinterpret_cast<decltype(g_kv_copy)>(p[6]);
+    g_kv_shared_rows = reinterpret_cast<decltype(g_kv_shared_rows)>(p[7]);
+    g_decode_shared = reinterpret_cast<decltype(g_decode_shared)>(p[8]);
     Py_RETURN_NONE;
 }
 
@@ -196,25 +206,95 @@ PyObject* qkv_prepare(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// decode(Q, O, cache address, cache device, table, lengths, scale, window, workspace, stream)
-PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 10, [&] {
-        const at::Tensor &Q = tensor(a[0], "Q"), &O = tensor(a[1], "O"), &workspace = tensor(a[8], "workspace");
-        const auto* cache = static_cast<const sawattn_kv_cache*>(pointer(a[2]));
+// What attn_decode and attn_decode_shared take alike: Q and O, [R, H, d], the cache, the table, the lengths, the workspace.
+struct DecodeTensors {
+    const at::Tensor &Q, &O, &workspace;
+    const sawattn_kv_cache* cache;
+    int device, out;
+    int64_t R;
+    DecodeTensors(PyObject* q, PyObject* o, PyObject* cache_at, PyObject* cache_device, PyObject* scratch)
+        : Q(tensor(q, "Q")), O(tensor(o, "O")), workspace(tensor(scratch, "workspace")), cache(static_cast<const sawattn_kv_cache*>(pointer(cache_at))) {
         if (!cache) refuse("cache", "given");
-        const int device = small(a[3], "cache device");
+        device = small(cache_device, "cache device");
         if (Q.dim() != 3 || device < 0 || device_of(Q) != device || input_type(Q) != cache->dtype || Q.stride(2) != 1 || Q.size(2) != cache->d ||
             Q.size(0) > INT32_MAX || Q.size(1) > INT32_MAX)
             refuse("Q", "a [R, H, d] tensor of the cache's device, dtype and d, contiguous in its last dimension");
-        const int out = O.scalar_type() == at::kFloat ? (int)SAWATTN_F32 : input_type(O);
+        out = O.scalar_type() == at::kFloat ? (int)SAWATTN_F32 : input_type(O);
         if (out < 0 || O.sizes() != Q.sizes() || device_of(O) != device || O.stride(2) != 1)
             refuse("O", "shaped like Q, on its device, contiguous in its last dimension (f16, bf16 or f32)");
         if (device_of(workspace) != device || !workspace.is_contiguous()) refuse("workspace", "a contiguous tensor on the other tensors' device");
-        const int64_t R = Q.size(0);
-        const PageTable table(a[4], R, device);
-        return launch(device, g_decode, static_cast<const void*>(Q.data_ptr()), Q.stride(0), Q.stride(1), O.data_ptr(), O.stride(0), O.stride(1), out, cache, table.at, table.stride, table.wide,
-                        flat<int32_t>(a[5], "lengths", at::kInt, R, device), (int)R, (int)Q.size(1), real(a[6]), small(a[7], "window"), workspace.data_ptr(),
-                        workspace.nbytes(), pointer(a[9]));
+        R = Q.size(0);
+    }
+};
+
+// decode(Q, O, cache address, cache device, table, lengths, scale, window, workspace, stream)
+PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 10, [&] {
+        const DecodeTensors t(a[0], a[1], a[2], a[3], a[8]);
+        const PageTable table(a[4], t.R, t.device);
+        return launch(t.device, g_decode, static_cast<const void*>(t.Q.data_ptr()), t.Q.stride(0), t.Q.stride(1), t.O.data_ptr(), t.O.stride(0), t.O.stride(1), t.out, t.cache,
+                      table.at, table.stride, table.wide, flat<int32_t>(a[5], "lengths", at::kInt, t.R, t.device), (int)t.R, (int)t.Q.size(1), real(a[6]),
+                      small(a[7], "window"), t.workspace.data_ptr(), t.workspace.nbytes(), pointer(a[9]));
+    });
+}
+
+// decode_shared(Q, O, cache address, cache device, table, lengths, group_offsets, shared, scale, workspace, stream)
+PyObject* decode_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 11, [&] {
+        const DecodeTensors t(a[0], a[1], a[2], a[3], a[9]);
+        const PageTable table(a[4], t.R, t.device);
+        const int64_t groups = tensor(a[7], "shared").numel();
+        if (groups >= INT32_MAX) refuse("shared", "of fewer than 2^31 - 1 elements");
+        return launch(t.device, g_decode_shared, static_cast<const void*>(t.Q.data_ptr()), t.Q.stride(0), t.Q.stride(1), t.O.data_ptr(), t.O.stride(0), t.O.stride(1), t.out,
+                      t.cache, table.at, table.stride, table.wide, flat<int32_t>(a[5], "lengths", at::kInt, t.R, t.device),
+                      flat<int32_t>(a[6], "group_offsets", at::kInt, groups + 1, t.device), flat<int32_t>(a[7], "shared", at::kInt, groups, t.device), (int)groups,
+                      (int)t.R, (int)t.Q.size(1), real(a[8]), t.workspace.data_ptr(), t.workspace.nbytes(), pointer(a[10]));
+    });
+}
+
+// kv_fork(lengths, source, rows, table, table_out, free_pages, free_state, lengths_out, copies, free_state_out, workspace, page_size, pages, stream)
+PyObject* kv_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 14, [&] {
+        const at::Tensor &lengths = tensor(a[0], "lengths"), &workspace = tensor(a[10], "workspace");
+        const int device = device_of(lengths);
+        if (device < 0) refuse("lengths", "a device tensor");
+        const int64_t R = lengths.numel(), N = tensor(a[1], "source").numel(), ring = tensor(a[5], "free_pages").numel();
+        if (R > INT32_MAX || N > INT32_MAX || ring > INT32_MAX) refuse("lengths, source and free_pages", "of fewer than 2^31 elements");
+        const PageTable table(a[3], R, device), table_out(a[4], N, device);
+        if (table.wide != table_out.wide) refuse("table_out", "as wide as the page table");
+        if (device_of(workspace) != device || !workspace.is_contiguous()) refuse("workspace", "a contiguous tensor on the other tensors' device");
+        const auto i32 = [&](int i, const char* name, int64_t size, bool optional = false) { return flat<int32_t>(a[i], name, at::kInt, size, device, optional); };
+        return launch(device, g_kv_fork, i32(0, "lengths", R), (int)R, i32(1, "source", N), i32(2, "rows", N, true), (int)N, table.at, table.stride, table_out.at,
+                      table_out.stride, table.wide, small(a[11], "page_size"), small(a[12], "pages"), i32(5, "free_pages", ring), (int)ring,
+                      i32(6, "free_state", 2), i32(7, "lengths_out", N), i32(8, "copies", 3 * N), i32(9, "free_state_out", 2), workspace.data_ptr(),
+                      workspace.nbytes(), pointer(a[13]));
+    });
+}
+
+// kv_copy(address of the caches, how many, their device, copies, stream)
+PyObject* kv_copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 5, [&] {
+        const auto* caches = static_cast<const sawattn_kv_cache*>(pointer(a[0]));
+        const int layers = small(a[1], "layers"), device = small(a[2], "cache device");
+        if (!caches || device < 0) refuse("caches", "given, on a device");
+        const int64_t count = tensor(a[3], "copies").numel() / 3;
+        if (count > INT32_MAX) refuse("copies", "of fewer than 2^31 rows");
+        return launch(device, g_kv_copy, caches, layers, flat<int32_t>(a[3], "copies", at::kInt, 3 * count, device), (int)count, pointer(a[4]));
+    });
+}
+
+// kv_shared_rows(lengths, table, group_offsets, shared, page_size, stream)
+PyObject* kv_shared_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 6, [&] {
+        const at::Tensor& lengths = tensor(a[0], "lengths");
+        const int device = device_of(lengths);
+        if (device < 0) refuse("lengths", "a device tensor");
+        const int64_t R = lengths.numel(), groups = tensor(a[3], "shared").numel();
+        if (R > INT32_MAX || groups >= INT32_MAX) refuse("lengths and shared", "of fewer than 2^31 - 1 elements");
+        const PageTable table(a[1], R, device);
+        return launch(device, g_kv_shared_rows, flat<int32_t>(a[0], "lengths", at::kInt, R, device), (int)R, table.at, table.stride, table.wide, small(a[4], "page_size"),
+                      flat<int32_t>(a[2], "group_offsets", at::kInt, groups + 1, device), (int)groups, flat<int32_t>(a[3], "shared", at::kInt, groups, device),
+                      pointer(a[5]));
     });
 }
 
@@ -222,6 +302,10 @@ PyMethodDef g_functions[] = {{"bind", reinterpret_cast<PyCFunction>(reinterpret_
                              {"kv_pages", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_pages)), METH_FASTCALL, nullptr},
                              {"qkv_prepare", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(qkv_prepare)), METH_FASTCALL, nullptr},
                              {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(decode)), METH_FASTCALL, nullptr},
+                             {"kv_fork", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_fork)), METH_FASTCALL, nullptr},
+                             {"kv_copy", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_copy)), METH_FASTCALL, nullptr},
+                             {"kv_shared_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(kv_shared_rows)), METH_FASTCALL, nullptr},
+                             {"decode_shared", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(decode_shared)), METH_FASTCALL, nullptr},
                              {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_paged", nullptr, -1, g_functions, nullptr, nullptr, nullptr, nullptr};
 

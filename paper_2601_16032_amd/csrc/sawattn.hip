@@ -6,3 +6,5 @@
 #include "attn_pages.hip"
 #include "attn_prepare.hip"
 #include "attn_decode.hip"
+#include "attn_fork.hip"
+#include "attn_shared.hip"
