@@ -472,7 +472,7 @@ int attn_kv_fork(const int32_t* lengths, int R, const int32_t* source, const int
                  const int32_t* free_state, int32_t* lengths_out, int32_t* copies, int32_t* free_state_out, void* workspace,
                  size_t workspace_bytes, void* hip_stream);
 
-/* attn_kv_fork_workspace_bytes -- the workspace attn_kv_fork needs: 2 bytes a page, 8 a new request and some; enough for fewer of each too. */
+/* attn_kv_fork_workspace_bytes -- the workspace attn_kv_fork needs: 2 bytes a page, 16 a new request and some; enough for fewer of each too. */
 int attn_kv_fork_workspace_bytes(int R, int N, int pages, size_t* bytes);
 
 /*
@@ -502,17 +502,17 @@ int attn_kv_shared_rows(const int32_t* lengths, int R, const int32_t* table, int
 /*
  * attn_decode_shared -- attn_decode for requests in groups that begin with the same rows, which are read once for a group.  Group g is the requests
  * group_offsets[g] .. group_offsets[g + 1] - 1.  Its requests have their first shared[g] rows in common, or as many of them as the shortest one
- * holds that is not empty, in whole pages; these are read where the table says so for the first request that is not empty, all others, and those
- * of requests in no group, where it says so for the request itself.
+ * holds that is not empty, in whole pages.  The tables of all of them must name pages that hold the same in these rows; which of them is read is left open.
  *
- *   Q .. scale      as in attn_decode.  R at most SAWATTN_MOST_REQUESTS, R*H*ceil(max_pages*page_size/128) below 2^31 - 2048.
+ *   Q .. scale      as in attn_decode.  R at most SAWATTN_MOST_REQUESTS, R*H*ceil(max_pages*page_size/32) below 2^31 - 8192.
  *   group_offsets   device, read: int32 [groups + 1], 1 <= groups <= SAWATTN_MOST_REQUESTS; outside 0 .. R they count as the nearest of these.
  *                   They must not fall; if they do, nothing is taken to be shared.
  *   shared          device, read: int32 [groups]; what attn_kv_shared_rows finds, or less
  *   workspace       device, written, 16-byte aligned, of at least attn_decode_shared_workspace_bytes; used by this call's kernels only
- * The result is that of attn_decode where the tables do name the same pages (or pages that hold the same), up to rounding: of the probabilities of shared rows 16 bits (bfloat16) or
- * 22 (binary16, ending at 2^-39 of the largest) enter the second product.  Requests of length 0, values that are infinite and pages that there are not as in
- * attn_decode (a bad page among the shared ones makes O of the whole group NaN).  The result does not depend on timing.  Two launches.  Stream and errors as attn_fwd.
+ * The result is that of attn_decode, up to rounding: of the probabilities 16 bits (bfloat16) or
+ * 22 (binary16, ending at 2^-35 of the largest) enter the second product.  Requests of length 0, values that are infinite and pages that there are not as in
+ * attn_decode (a bad page among the shared ones may make O of the whole group NaN; an infinity meets NaN where its probability is less than 2^-35 of the largest).  The result does not depend on timing.
+ * Two launches; where R*cache->heads*max_pages*page_size*d are few, up to 12 million or 50 million, those of attn_decode.  Stream and errors as attn_fwd.
  */
 int attn_decode_shared(const void* Q, int64_t q_request, int64_t q_head, void* O, int64_t o_request, int64_t o_head, int o_dtype,
                        const sawattn_kv_cache* cache, const int32_t* table, int64_t table_stride, int max_pages, const int32_t* lengths,
@@ -520,7 +520,7 @@ int attn_decode_shared(const void* Q, int64_t q_request, int64_t q_head, void* O
                        size_t workspace_bytes, void* hip_stream);
 
 /* attn_decode_shared_workspace_bytes -- the workspace attn_decode_shared needs for R requests of H heads in `groups` groups: 2 d R H floats and at most some
- * 44 MiB.  The same workspace does for every call of as many requests and groups or fewer.  Launches nothing. */
+ * 110 MiB, or what attn_decode needs.  The same workspace does for every call of as many requests and groups or fewer.  Launches nothing. */
 int attn_decode_shared_workspace_bytes(const sawattn_kv_cache* cache, int R, int H, int groups, int max_pages, size_t* bytes);
 
 /* Text of the last error raised on the calling thread ("" if none).  Static storage, never NULL. */

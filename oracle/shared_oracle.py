@@ -55,18 +55,3 @@ def shared_rows(table, lengths, offsets, page_size):
             n += 1
         out.append(n * page_size)
     return out
-
-
-def common_rows(lengths, offsets, shared, page_size, R):
-    """Per request: (first rows that it has in common with its group, the request whose table row names their pages), as attn_decode_shared takes it."""
-    out = [(0, r) for r in range(R)]
-    at = [min(max(int(x), 0), R) for x in offsets]
-    if any(a > b for a, b in zip(at, at[1:])):
-        return out
-    for g, (a, b) in enumerate(zip(at, at[1:])):
-        mine = [r for r in range(a, b) if lengths[r] > 0]
-        if b - a > 1 and mine:
-            n = max(min([int(shared[g])] + [int(lengths[r]) for r in mine]), 0) // page_size * page_size
-            for r in mine:
-                out[r] = (n, mine[0])
-    return out

@@ -545,8 +545,8 @@ def attn_decode_shared_workspace_bytes(R: int, H: int, groups: int, cache: KVCac
 
 
 def attn_decode_shared(Q, cache: KVCache, table, lengths, group_offsets, shared, O=None, *, scale: float, o_dtype=None, workspace=None, stream=None):
-    """attn_decode for requests in groups: the first shared[g] rows of the requests group_offsets[g] .. group_offsets[g + 1] - 1 are read once, by the table row
-    of the first of them.  workspace: a uint8 tensor of at least attn_decode_shared_workspace_bytes bytes, made here when None.  Returns O without waiting."""
+    """attn_decode for requests in groups: the first shared[g] rows of the requests group_offsets[g] .. group_offsets[g + 1] - 1 are the same, and
+    read once.  workspace: a uint8 tensor of at least attn_decode_shared_workspace_bytes bytes, made here when None.  Returns O without waiting."""
     if O is None:
         O = _empty(Q.shape, o_dtype or Q.dtype, Q.device, stream)
     if workspace is None:

@@ -631,6 +631,18 @@ int decode_params(const void* Q, int64_t q_request, int64_t q_head, void* O, int
     return SAWATTN_OK;
 }
 
+// Launches what decode_params has filled in; workspace: of decode_bytes, NULL where that is 0.
+int run_decode(DecodeParams& p, const DecodePlan& plan, int H, int d, int dtype, void* workspace, hipStream_t stream) {
+    if (workspace) {
+        p.parts = static_cast<float*>(workspace);
+        p.begun = reinterpret_cast<int4*>(p.parts + (size_t)2 * plan.grid * plan.heads_kept * d);
+        p.part_sums = reinterpret_cast<f2*>(p.begun + plan.grid);
+    }
+    const bool bf = dtype == SAWATTN_BF16;
+    if (d == 128) return bf ? launch_decode<128, true>(p, plan, H, stream) : launch_decode<128, false>(p, plan, H, stream);
+    return bf ? launch_decode<64, true>(p, plan, H, stream) : launch_decode<64, false>(p, plan, H, stream);
+}
+
 }  // namespace sawattn
 
 extern "C" {
@@ -670,16 +682,7 @@ int attn_decode(const void* Q, int64_t q_request, int64_t q_head, void* O, int64
     rc = decode_params(Q, q_request, q_head, O, o_request, o_head, o_dtype, cache, table, table_stride, max_pages, lengths, R, H, scale, window, workspace,
                        workspace_bytes, need, plan, &p);
     if (rc != SAWATTN_OK) return rc;
-    const int d = cache->d;
-    if (need) {
-        p.parts = static_cast<float*>(workspace);
-        p.begun = reinterpret_cast<int4*>(p.parts + (size_t)2 * plan.grid * plan.heads_kept * d);
-        p.part_sums = reinterpret_cast<f2*>(p.begun + plan.grid);
-    }
-    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const bool bf = cache->dtype == SAWATTN_BF16;
-    if (d == 128) return bf ? launch_decode<128, true>(p, plan, H, stream) : launch_decode<128, false>(p, plan, H, stream);
-    return bf ? launch_decode<64, true>(p, plan, H, stream) : launch_decode<64, false>(p, plan, H, stream);
+    return run_decode(p, plan, H, cache->d, cache->dtype, need ? workspace : nullptr, static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"

@@ -8,12 +8,14 @@
 // list of copies.  Fresh pages are dealt out in the order of the requests, pages given back in the order of their numbers: nothing depends on timing.
 //
 // Bound by latency: a few numbers per request, four bytes per table entry in and out.  Three launches (numbers of requests; tables and marks; pages
-// given back), each of which needs all of the one before.
+// given back), each of which needs all of the one before; one where all tables together are short (kv_fork_few_kernel: 8 requests of 125 pages 4.6 us, in three
+// launches 2.6 + 3.0 + 3.9).  1000 requests of up to 512 pages 4.1 + 4.2 + 4.3 us, 100 that become 4000 of up to 1024 pages 11 + 6 + 2.4.
 namespace sawattn {
 
 constexpr int kForkThreads = 1024, kForkEach = SAWATTN_MOST_REQUESTS / kForkThreads;      // requests of a thread at most
 constexpr int kForkTableThreads = 256, kForkRow = 4 * kForkTableThreads;                   // table entries of a workgroup
 constexpr int kForkPages = 16 * kForkThreads;                                              // pages of a workgroup, 16 marks of a thread
+constexpr int kForkFewRequests = kForkThreads, kForkFewPages = 1 << 17, kForkFewEntries = 1 << 14;      // of a call that one workgroup does all of, at most
 
 struct ForkParams {
     const int* lengths;
@@ -29,14 +31,39 @@ struct ForkParams {
     int* state_out;
     u4* kept;                 // workspace: a byte for every page, not 0 if a new request holds it
     u4* held;                 // ... if an old one does
-    int2* plan;               // [N] (entries taken from the source, fresh page behind them or -1)
+    int4* plan;               // [N], ForkPlan
     int2* taken;              // (pages taken from the ring, pages that were in it)
     int R, N, max_pages, shift, pages, ring_size, mark_words;      // words of 16 marks
+};
+
+struct ForkPlan {      // of a new request
+    int count;         // entries taken from its source
+    int fresh;         // the fresh page's entry behind them, or -1
+    int page;          // that page
+    int marked;        // entries that another request of the same source marks
 };
 
 __device__ __forceinline__ int fork_length(const ForkParams& p, int s) {
     return (int)min((long long)max(p.lengths[s], 0), (long long)p.max_pages << p.shift);
 }
+
+// Where the ring begins and how much is in it, whatever is given; and a place `i` behind its first one, i at most twice its size.
+struct ForkRing {
+    unsigned first, size;
+    int available;
+    __device__ __forceinline__ ForkRing(const ForkParams& p) {
+        const int first_given = p.state[0], free_given = p.state[1];
+        size = (unsigned)p.ring_size;
+        first = first_given >= 0 && (unsigned)first_given < size ? (unsigned)first_given : 0u;
+        available = min(max(free_given, 0), p.ring_size);
+    }
+    __device__ __forceinline__ unsigned at(unsigned long long i) const {
+        i += first;
+        if (i >= size) i -= size;
+        if (i >= size) i -= size;
+        return (unsigned)i;
+    }
+};
 
 // Sum over the threads in front of this one, and over all.
 __device__ __forceinline__ int block_before(int x, int (&of_wave)[kForkThreads / 64], int& all) {
@@ -53,9 +80,89 @@ __device__ __forceinline__ int block_before(int x, int (&of_wave)[kForkThreads /
     return before;
 }
 
+// What every request holds, EACH of them worked out by a thread; keep(r, plan) gets the plans.  winner, lead, counts: LDS, an entry for every old request.  Returns the pages taken.
+template <int EACH, typename KEEP>
+__device__ __forceinline__ int fork_requests(const ForkParams& p, const ForkRing& ring, int* winner, int* lead, int* counts, int (&of_wave)[kForkThreads / 64], KEEP&& keep) {
+    const int tid = threadIdx.x, each = (p.N + kForkThreads - 1) / kForkThreads, r0 = tid * each, in_page = (1 << p.shift) - 1;
+    int s[EACH], rows[EACH], length[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const bool there = i < each && r0 + i < p.N;
+        s[i] = there ? p.source[r0 + i] : -1;
+        rows[i] = there && p.rows ? max(p.rows[r0 + i], 0) : 0x7fffffff;
+        if (s[i] >= p.R) s[i] = -1;
+    }
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) length[i] = s[i] >= 0 ? fork_length(p, s[i]) : 0;
+    for (int i = tid; i < p.R; i += kForkThreads) winner[i] = lead[i] = p.N;
+    __syncthreads();
+    bool last[EACH];      // ends in its source's part-filled page: the first such request takes it over
+    int own_s = -1, own_last = -1;      // sources of the thread's last request, and of that if it is such a one
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        rows[i] = min(rows[i], length[i]);
+        last[i] = (rows[i] & in_page) && rows[i] >> p.shift == length[i] >> p.shift;
+        if (i < each) {
+            own_s = s[i];
+            own_last = last[i] ? s[i] : -1;
+        }
+    }
+    // (the first of neighbours with the same source speaks for them: atomics on one place go one after the other)
+    int before_s = __shfl_up(own_s, 1), before_last = __shfl_up(own_last, 1);
+    if ((tid & 63) == 0) before_s = before_last = -1;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (s[i] >= 0 && s[i] != before_s) atomicMin(&lead[s[i]], r0 + i);
+        if (last[i] && s[i] != before_last) atomicMin(&winner[s[i]], r0 + i);
+        before_s = s[i];
+        before_last = last[i] ? s[i] : -1;
+    }
+    __syncthreads();
+    int missing = 0;
+    bool misses[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (last[i]) last[i] = winner[s[i]] == r0 + i;
+        misses[i] = (rows[i] & in_page) && !last[i];
+        missing += misses[i];
+    }
+    int all;
+    int before = block_before(missing, of_wave, all);
+    int count[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const bool ok = !misses[i] || before < ring.available;
+        count[i] = ok ? (rows[i] >> p.shift) + last[i] : 0;
+        before += misses[i];
+        if (s[i] >= 0 && lead[s[i]] == r0 + i) counts[s[i]] = count[i];
+    }
+    __syncthreads();
+    before -= missing;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int r = r0 + i;
+        if (i >= each || r >= p.N) continue;
+        const int full = rows[i] >> p.shift;
+        int from = -1, to = -1;
+        bool ok = true;
+        if (misses[i]) {
+            ok = before < ring.available;
+            from = p.table[s[i] * p.table_stride + full];
+            if (ok) to = p.ring[ring.at((unsigned)before)];
+            ++before;
+        }
+        p.lengths_out[r] = ok ? rows[i] : 0;
+        p.copies[3 * r] = from;
+        p.copies[3 * r + 1] = to;
+        p.copies[3 * r + 2] = misses[i] ? rows[i] & in_page : 0;
+        keep(r, ForkPlan{count[i], misses[i] && ok ? full : -1, to, s[i] >= 0 && lead[s[i]] != r ? counts[s[i]] : 0});
+    }
+    return min(all, ring.available);
+}
+
 // The first workgroup works out what every request holds, the others clear the marks.
 __global__ __launch_bounds__(kForkThreads) void kv_fork_kernel(ForkParams p) {
-    __shared__ int winner[SAWATTN_MOST_REQUESTS];      // the request that takes over the source's part-filled page
+    __shared__ int winner[SAWATTN_MOST_REQUESTS], lead[SAWATTN_MOST_REQUESTS], counts[SAWATTN_MOST_REQUESTS];
     __shared__ int of_wave[kForkThreads / 64];
     const int tid = threadIdx.x;
     if (blockIdx.x) {
@@ -63,96 +170,42 @@ __global__ __launch_bounds__(kForkThreads) void kv_fork_kernel(ForkParams p) {
             p.kept[i] = p.held[i] = u4{0, 0, 0, 0};
         return;
     }
-    const unsigned F = (unsigned)p.ring_size;
-    const int first_given = p.state[0], free_given = p.state[1];
-    const int each = (p.N + kForkThreads - 1) / kForkThreads, r0 = tid * each;
-    int s[kForkEach], rows[kForkEach], length[kForkEach];
-#pragma unroll
-    for (int i = 0; i < kForkEach; ++i) {
-        const bool there = i < each && r0 + i < p.N;
-        s[i] = there ? p.source[r0 + i] : -1;
-        rows[i] = there && p.rows ? max(p.rows[r0 + i], 0) : 0x7fffffff;
-        if (s[i] >= p.R) s[i] = -1;
-    }
-#pragma unroll
-    for (int i = 0; i < kForkEach; ++i) length[i] = s[i] >= 0 ? fork_length(p, s[i]) : 0;
-    for (int i = tid; i < p.R; i += kForkThreads) winner[i] = p.N;
-    __syncthreads();
-    const int in_page = (1 << p.shift) - 1;
-    bool last[kForkEach];      // ends in its source's part-filled page
-#pragma unroll
-    for (int i = 0; i < kForkEach; ++i) {
-        rows[i] = min(rows[i], length[i]);
-        last[i] = (rows[i] & in_page) && rows[i] >> p.shift == length[i] >> p.shift;
-        if (last[i]) atomicMin(&winner[s[i]], r0 + i);
-    }
-    __syncthreads();
-    int missing = 0;
-    bool misses[kForkEach];
-#pragma unroll
-    for (int i = 0; i < kForkEach; ++i) {
-        if (last[i]) last[i] = winner[s[i]] == r0 + i;
-        misses[i] = (rows[i] & in_page) && !last[i];
-        missing += misses[i];
-    }
-    int all;
-    int before = block_before(missing, of_wave, all);
-    const unsigned first = first_given >= 0 && (unsigned)first_given < F ? (unsigned)first_given : 0u;
-    const int available = min(max(free_given, 0), p.ring_size);
-#pragma unroll
-    for (int i = 0; i < kForkEach; ++i) {
-        const int r = r0 + i;
-        if (i >= each || r >= p.N) continue;
-        const int full = rows[i] >> p.shift;
-        int from = -1, to = -1, left = 0;
-        bool ok = true;
-        if (misses[i]) {
-            ok = before < available;
-            from = p.table[s[i] * p.table_stride + full];
-            left = rows[i] & in_page;
-            if (ok) to = p.ring[((unsigned long long)first + (unsigned)before) % F];
-            ++before;
-        }
-        p.lengths_out[r] = ok ? rows[i] : 0;
-        p.copies[3 * r] = from;
-        p.copies[3 * r + 1] = to;
-        p.copies[3 * r + 2] = left;
-        p.plan[r] = int2{ok ? full + last[i] : 0, misses[i] && ok ? full : -1};
-    }
-    if (tid == 0) *p.taken = int2{min(all, available), available};
+    const ForkRing ring(p);
+    const int taken = fork_requests<kForkEach>(p, ring, winner, lead, counts, of_wave, [&](int r, const ForkPlan& x) { p.plan[r] = int4{x.count, x.fresh, x.page, x.marked}; });
+    if (tid == 0) *p.taken = int2{taken, ring.available};
 }
 
 // Tables: a workgroup takes kForkRow entries of one request.  First the old batch's, whose pages it marks as held, then the new one's.  (What
-// several workgroups mark, they mark alike.)
+// several workgroups mark, they mark alike; of the requests of one source mostly the first does it for all: a mark is a line of the L2 to itself, 100 prompts that become
+// 4000 requests of up to 1024 pages 9.2 -> 6.2 us.)
 __global__ __launch_bounds__(kForkTableThreads) void kv_fork_table_kernel(ForkParams p, int parts) {
     const int item = blockIdx.x / parts, from = (int)(blockIdx.x - item * parts) * kForkRow + threadIdx.x;
     constexpr int kEach = kForkRow / kForkTableThreads;
     const bool old = item < p.R;
     const int r = old ? item : item - p.R;
     unsigned char* const marks = reinterpret_cast<unsigned char*>(old ? p.held : p.kept);
-    int s, count;
-    int2 plan = {0, -1};
+    int s;
+    int4 plan = {0, -1, 0, 0};
     if (old) {
         s = r;
-        count = (int)(((long long)fork_length(p, r) + (1 << p.shift) - 1) >> p.shift);
+        plan.x = (int)(((long long)fork_length(p, r) + (1 << p.shift) - 1) >> p.shift);
     } else {
         s = p.source[r];
         plan = p.plan[r];
-        count = plan.x;
     }
     const int* const row = p.table + s * p.table_stride;
     int* const out = p.table_out + r * p.out_stride;
     int page[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) page[i] = from + i * kForkTableThreads < count ? row[from + i * kForkTableThreads] : -1;
+    for (int i = 0; i < kEach; ++i) page[i] = from + i * kForkTableThreads < plan.x ? row[from + i * kForkTableThreads] : -1;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const int j = from + i * kForkTableThreads;
-        if (j < count) {
-            if ((unsigned)page[i] < (unsigned)p.pages) marks[page[i]] = 1;
+        if (j < plan.x) {
+            if (j >= plan.w && (unsigned)page[i] < (unsigned)p.pages) marks[page[i]] = 1;
             if (!old) out[j] = page[i];
         }
-        if (!old && j == plan.y) out[j] = p.copies[3 * r + 1];
+        if (!old && j == plan.y) out[j] = plan.z;
     }
 }
 
@@ -168,34 +221,86 @@ __global__ __launch_bounds__(kForkThreads) void kv_fork_free_kernel(ForkParams p
     auto count = [](u4 m) { return __popc(m[0]) + __popc(m[1]) + __popc(m[2]) + __popc(m[3]); };
     const u4 mine = freed(blockIdx.x * kForkThreads + tid);
     const int2 taken = *p.taken;
+    const ForkRing ring(p);
     int in_front = 0;
 #pragma unroll 4
     for (unsigned c = 0; c < blockIdx.x; ++c) in_front += count(freed(c * kForkThreads + tid));
     int front, own;
     block_before(in_front, of_wave[0], front);
     int before = front + block_before(count(mine), of_wave[1], own);
-    const unsigned F = (unsigned)p.ring_size;
-    const int given = p.state[0];
-    const unsigned first = given >= 0 && (unsigned)given < F ? (unsigned)given : 0u;
     const int room = p.ring_size - taken.y;      // (there is room for all of them if the ring has a place for every page)
+    if (count(mine))
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
+        for (int w = 0; w < 4; ++w)
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
-            if (mine[w] >> (8 * b) & 1) {
-                if (before < room) p.ring[((unsigned long long)first + (unsigned)taken.y + (unsigned)before) % F] = (blockIdx.x * kForkThreads + tid) * 16 + w * 4 + b;
-                ++before;
-            }
+            for (int b = 0; b < 4; ++b)
+                if (mine[w] >> (8 * b) & 1) {
+                    if (before < room) p.ring[ring.at((unsigned long long)taken.y + (unsigned)before)] = (blockIdx.x * kForkThreads + tid) * 16 + w * 4 + b;
+                    ++before;
+                }
     if (blockIdx.x == gridDim.x - 1 && tid == 0) {
-        p.state_out[0] = (int)(((unsigned long long)first + (unsigned)taken.x) % F);
+        p.state_out[0] = (int)ring.at((unsigned)taken.x);
         p.state_out[1] = (int)min((long long)taken.y - taken.x + front + own, (long long)p.ring_size);
+    }
+}
+
+// All of it in one workgroup, the marks in LDS, a bit to a page: for few and short tables, where the launches take longer than the work.
+__global__ __launch_bounds__(kForkThreads) void kv_fork_few_kernel(ForkParams p) {
+    __shared__ int winner[kForkFewRequests], lead[kForkFewRequests], counts[kForkFewRequests], of_wave[kForkThreads / 64], of_wave_freed[kForkThreads / 64];
+    __shared__ ForkPlan plan[kForkFewRequests];
+    extern __shared__ unsigned marks[];      // held, kept
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, words = (p.pages + 31) / 32, each = (words + kForkThreads - 1) / kForkThreads;
+    unsigned* const held = marks;
+    unsigned* const kept = marks + words;
+    const ForkRing ring(p);
+    for (int i = tid; i < 2 * words; i += kForkThreads) marks[i] = 0;
+    const int taken = fork_requests<1>(p, ring, winner, lead, counts, of_wave, [&](int r, const ForkPlan& x) { plan[r] = x; });
+    __syncthreads();
+    for (int item = wave; item < p.R + p.N; item += kForkThreads / 64) {
+        const bool old = item < p.R;
+        const int r = old ? item : item - p.R;
+        ForkPlan x = {0, -1, 0, 0};
+        if (old) x.count = (int)(((long long)fork_length(p, r) + (1 << p.shift) - 1) >> p.shift);
+        else x = plan[r];
+        const int* const row = p.table + (old ? r : p.source[r]) * p.table_stride;
+        int* const out = p.table_out + r * p.out_stride;
+        unsigned* const bits = old ? held : kept;
+#pragma unroll 4
+        for (int j = lane; j < x.count; j += 64) {
+            const int page = row[j];
+            if (j >= x.marked && (unsigned)page < (unsigned)p.pages) atomicOr(&bits[page / 32], 1u << page % 32);
+            if (!old) out[j] = page;
+        }
+        if (!old && lane == 0 && x.fresh >= 0) out[x.fresh] = x.page;
+    }
+    __syncthreads();
+    int mine = 0;
+    for (int i = 0; i < each; ++i) {
+        const int word = tid * each + i;
+        if (word < words) mine += __popc(held[word] & ~kept[word]);
+    }
+    int all;
+    int before = block_before(mine, of_wave_freed, all);
+    const int room = p.ring_size - ring.available;
+    for (int i = 0; mine && i < each; ++i) {
+        const int word = tid * each + i;
+        for (unsigned bits = word < words ? held[word] & ~kept[word] : 0u; bits; bits &= bits - 1) {
+            if (before < room) p.ring[ring.at((unsigned long long)ring.available + (unsigned)before)] = word * 32 + __builtin_ctz(bits);
+            ++before;
+        }
+    }
+    if (tid == 0) {
+        p.state_out[0] = (int)ring.at((unsigned)taken);
+        p.state_out[1] = (int)min((long long)ring.available - taken + all, (long long)p.ring_size);
     }
 }
 
 // ---- copies
 //
 // A row of a head is d elements side by side; of a copy there are heads * rows of them in each of K and V of each layer.  They are dealt out in
-// pieces of kCopyRows, counted through all copies by a sum that every workgroup makes for itself (entries that are none cost nothing behind it).
+// pieces of 64 rows (128 at d = 64), counted through all copies by a sum that every workgroup makes for itself (entries that are none cost nothing behind it).
+// Bound by memory: 121 pages of 64 rows and fewer, 8 heads of 128, in 16 layers, 242 MB read and written, 54 us, 4.5 TB/s (20 us of it at twice
+// that rate if all came from the Infinity Cache); loaded and stored cached 57.5.
 constexpr int kCopyThreads = 256, kCopyLayers = 32, kCopyEach = SAWATTN_MOST_REQUESTS / kCopyThreads;
 constexpr int kCopyAhead = 4;      // 16-byte pieces of a thread on their way
 
@@ -263,27 +368,28 @@ __global__ __launch_bounds__(kCopyThreads) void kv_copy_kernel(CopyParams p) {
         for (int i = 0; i < kCopyAhead; ++i) {
             const int flat = first + i * kRows + tid / kLanes, head = (unsigned)flat / (unsigned)max(rows, 1), row = flat - head * rows;
             where[i] = head < p.heads && rows ? head * l.head[v] + row * l.row[v] + tid % kLanes * 16 : -1;
-            if (where[i] >= 0) x[i] = *reinterpret_cast<const u4*>(source + where[i]);
+            if (where[i] >= 0) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u4*>(source + where[i]));
         }
 #pragma unroll
         for (int i = 0; i < kCopyAhead; ++i)
-            if (where[i] >= 0) *reinterpret_cast<u4*>(target + where[i]) = x[i];
+            if (where[i] >= 0) __builtin_nontemporal_store(x[i], reinterpret_cast<u4*>(target + where[i]));
     }
 }
 
 // ---- common rows
 //
-// A workgroup to a group; a thread to a table column, of which it looks at all requests' entries, eight on their way at a time.
-constexpr int kCommonThreads = 1024, kCommonAhead = 8;
+// A workgroup to a group; a thread to a table column, of which it looks at all requests' entries, sixteen on their way at a time.
+constexpr int kCommonThreads = 1024, kCommonAhead = 16;
 
 __global__ __launch_bounds__(kCommonThreads) void kv_shared_rows_kernel(const int* lengths, const int* table, long long stride, int max_pages, int shift,
                                                                       const int* offsets, int R, int* shared) {
-    __shared__ int least, lead, differ;
+    __shared__ int least, count, differ;
+    __shared__ unsigned short there[SAWATTN_MOST_REQUESTS];      // the requests that hold a row, in any order
     const int tid = threadIdx.x, g = blockIdx.x;
     const int begin = min(max(offsets[g], 0), R), end = min(max(offsets[g + 1], 0), R);
     if (tid == 0) {
         least = 0x7fffffff;
-        lead = R;
+        count = 0;
         differ = max_pages;
     }
     __syncthreads();
@@ -291,30 +397,23 @@ __global__ __launch_bounds__(kCommonThreads) void kv_shared_rows_kernel(const in
         const int length = lengths[r];
         if (length > 0) {
             atomicMin(&least, length);
-            atomicMin(&lead, r);
+            there[atomicAdd(&count, 1)] = (unsigned short)r;
         }
     }
     __syncthreads();
-    if (lead == R) {      // no request that holds a row
-        if (tid == 0) shared[g] = 0;
-        return;
-    }
-    const int pages = min(least >> shift, max_pages);
+    const int n = count;
+    const int pages = n ? min(least >> shift, max_pages) : 0;
     for (int j0 = 0; j0 < pages; j0 += kCommonThreads) {
         const int j = j0 + tid;
         if (j < pages) {
-            const int page = table[lead * stride + j];
+            const int page = table[there[0] * stride + j];
             bool same = true;
-            for (int r = lead + 1; r < end; r += kCommonAhead) {
-                int other[kCommonAhead], length[kCommonAhead];
+            for (int i0 = 1; i0 < n; i0 += kCommonAhead) {
+                int other[kCommonAhead];
 #pragma unroll
-                for (int i = 0; i < kCommonAhead; ++i) {
-                    const int at = min(r + i, end - 1);
-                    other[i] = table[at * stride + j];
-                    length[i] = lengths[at];
-                }
+                for (int i = 0; i < kCommonAhead; ++i) other[i] = table[there[min(i0 + i, n - 1)] * stride + j];
 #pragma unroll
-                for (int i = 0; i < kCommonAhead; ++i) same = same && (other[i] == page || length[i] <= 0);
+                for (int i = 0; i < kCommonAhead; ++i) same = same && other[i] == page;
             }
             if (!same) atomicMin(&differ, j);
         }
@@ -331,7 +430,7 @@ struct ForkWorkspace {      // bytes, from the front
         const size_t marks = ((size_t)pages + 15) / 16 * 16;
         held = marks;
         plan = 2 * marks;
-        taken = plan + sizeof(int2) * (size_t)N;
+        taken = plan + sizeof(int4) * (size_t)N;
         all = taken + sizeof(int2);
     }
 };
@@ -386,9 +485,14 @@ int attn_kv_fork(const int32_t* lengths, int R, const int32_t* source, const int
     const ForkWorkspace at(N, pages);
     char* const w = static_cast<char*>(workspace);
     ForkParams p = {lengths, source, rows, table, table_out, table_stride, table_out_stride, free_pages, free_state, lengths_out, copies, free_state_out,
-                    reinterpret_cast<u4*>(w), reinterpret_cast<u4*>(w + at.held), reinterpret_cast<int2*>(w + at.plan), reinterpret_cast<int2*>(w + at.taken),
+                    reinterpret_cast<u4*>(w), reinterpret_cast<u4*>(w + at.held), reinterpret_cast<int4*>(w + at.plan), reinterpret_cast<int2*>(w + at.taken),
                     R, N, max_pages, page_shift(page_size), pages, ring, (int)(((long long)pages + 15) / 16)};
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (R <= kForkFewRequests && N <= kForkFewRequests && pages <= kForkFewPages && (long long)(R + N) * max_pages <= kForkFewEntries) {
+        const int words = (pages + 31) / 32;
+        hipLaunchKernelGGL(kv_fork_few_kernel, dim3(1), dim3(kForkThreads), 2 * words * sizeof(unsigned), stream, p);
+        return launched("attn_kv_fork");
+    }
     const int clearing = std::min(255, (p.mark_words + kForkThreads - 1) / kForkThreads);
     hipLaunchKernelGGL(kv_fork_kernel, dim3(1 + clearing), dim3(kForkThreads), 0, stream, p);
     int status = launched("attn_kv_fork");

@@ -19,8 +19,8 @@ constexpr float kRescaleSlack = 8.0f;
 // |M| = 2^24 the distance is larger than the slack, and a limit below t would let a smaller maximum than the present one
 // lower the reference -- O and the running sum would grow by a power of two each time, without bound.  (fmaxf also
 // ignores the NaN of an infinite M: then only a larger score, that is none, asks for another raise.)
-SAW_HD float score_limit(float t, float M, float c) {
-    return fmaxf(t, (M + kRescaleSlack - fabsf(M) * 0x1p-21f) / c);
+SAW_HD float score_limit(float t, float M, float c, float slack = kRescaleSlack) {
+    return fmaxf(t, (M + slack - fabsf(M) * 0x1p-21f) / c);
 }
 
 }  // namespace sawattn
