@@ -610,3 +610,270 @@ def test_decode_shared_far_into_a_large_cache():
     want = attend(small, q, 0.1)
     got = binding.attn_decode_shared(q, binding.KVCache(k, v), widened(cache, table + far), up(lengths), offsets, shared, scale=0.1)
     assert torch.equal(got, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,below", [("f16", 30), ("bf16", 30), ("bf16", 60)])
+@pytest.mark.parametrize("G", [1, 9])
+def test_decode_shared_infinite_values_of_small_weight(dtype, below, G):
+    """An infinite value whose probability is 2^-30 of the largest (bfloat16: 2^-60) makes its element infinite, among the rows in common and behind them."""
+    d, n = 128, 1024
+    case = fill_groups([(n, [40, 50, 60, 70])], [], 1, d, 16, dtype, seed=9)
+    cache, table, lengths, offsets, shared, _ = case
+    q = torch.zeros(4, G, d, dtype=DTYPES[dtype], device="cuda")
+    q[:, :, 3] = 1.0
+    cache.k[:, :, :, 3] = 0.0
+    scale = math.log(2.0) / 8      # a key of 8 x in element 3 has a score of x in powers of two
+    cache.k[int(table[0, 10]), 0, 7, 3], cache.v[int(table[0, 10]), 0, 7, 5] = -8.0 * below, math.inf
+    cache.k[int(table[1, n // 16 + 1]), 0, 2, 3], cache.v[int(table[1, n // 16 + 1]), 0, 2, 6] = -8.0 * below, -math.inf
+    got = attend(case, q, scale)
+    assert (got[:, :, 5] == math.inf).all() and (got[1, :, 6] == -math.inf).all()
+    got[:, :, 5], got[1, :, 6] = 0, 0
+    assert got.isfinite().all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("G", [1, 5, 40])
+def test_decode_shared_rising_scores(dtype, G):
+    """Scores that rise from tile to tile by less and by more than what a reference is raised for, and fall again."""
+    d, n = 64, 2048
+    case = fill_groups([(n, [100, 100, 3])], [], 1, d, 16, dtype, seed=11)
+    cache, table, lengths, offsets, shared, keys = case
+    q = queries(3, G, d, dtype, seed=12)
+    q[:, :, 0] = 1.0
+    level = 10.0 * torch.sin(torch.arange(n + 100, device="cuda") / 300.0) + 6.0 * torch.sin(torch.arange(n + 100, device="cuda") / 7.0)
+    for r in range(3):
+        m = lengths[r]
+        keys[0][r][:, 0, 0] = level[:m].to(q.dtype)
+        rows = torch.arange(m, device="cuda")
+        cache.k[table[r, rows // 16].long(), 0, rows % 16, 0] = keys[0][r][:, 0, 0]
+    check_shared(attend(case, q, 1.0, o_dtype=torch.float32), q, keys, 1.0, lengths, dtype)
+
+
+# ------------------------------------------------------------------------------------------- all of them together
+
+class Beams:
+    """A search as a program runs it: prompts, beams that branch off them, and per step a fork by given sources, copies, a token each, attention; and what
+    every beam's keys and values are, on the host."""
+
+    def __init__(self, prompts, beams, H, KH, d, ps, dtype, seed, wide):
+        self.H, self.KH, self.d, self.ps, self.beams, self.wide = H, KH, d, ps, beams, wide
+        self.R = R = len(prompts) * beams
+        self.pages = 4 * R + sum(-(-(n + 400) // ps) for n in prompts) * 2 + R * 8
+        g = torch.Generator("cuda").manual_seed(seed)
+        dt = DTYPES[dtype]
+        self.layers = [binding.KVCache(*(torch.full((self.pages, KH, ps, d), float("nan"), dtype=dt, device="cuda") for _ in range(2))) for _ in range(2)]
+        self.both = binding.KVLayers(self.layers)
+        self.ring, state = torch.randperm(self.pages, generator=g, device="cuda").int(), up([0, self.pages])
+        # the prompts, in every layer
+        table, lengths, n = torch.full((len(prompts), wide), POISON, dtype=torch.int32, device="cuda"), up([0] * len(prompts)), sum(prompts)
+        page = binding.attn_kv_pages(lengths, up(prompts), table, self.ring, state, page_size=ps, tokens=n)
+        self.history = [[None] * R for _ in self.layers]
+        for cache, kept in zip(self.layers, self.history):
+            qkv = torch.randn(n, H + 2 * KH, d, generator=g, device="cuda").to(dt)
+            q, k, v = qkv.split((H, KH, KH), 1)
+            binding.attn_qkv_prepare(q, k, v, positions=page.positions, cache=cache, slots=page.slots)
+            at = np.concatenate([[0], np.cumsum(prompts)])
+            for r in range(R):
+                p = r // beams
+                kept[r] = (k[at[p]:at[p + 1]].clone(), v[at[p]:at[p + 1]].clone())
+        self.offsets = up(np.arange(len(prompts) + 1) * beams)
+        # two sets of what a fork writes beside what it reads
+        self.sets = [dict(table=torch.full((R, wide), POISON, dtype=torch.int32, device="cuda"), lengths=up([0] * R), state=up([0, 0])) for _ in range(2)]
+        start = binding.attn_kv_fork(page.lengths, up(np.repeat(np.arange(len(prompts)), beams)), table, self.ring, page.free_state, page_size=ps, pages=self.pages,
+                                     table_out=self.sets[0]["table"], lengths_out=self.sets[0]["lengths"], free_state_out=self.sets[0]["state"])
+        binding.attn_kv_copy(self.both, start.copies)
+        self.workspace = [torch.full((binding.attn_decode_shared_workspace_bytes(R, H, len(prompts), self.layers[0], wide),), 0xff, dtype=torch.uint8, device="cuda"),
+                          torch.full((binding.attn_kv_fork_workspace_bytes(R, R, self.pages),), 0xff, dtype=torch.uint8, device="cuda")]
+        self.one = up([1] * R)
+
+    def step(self, which, source, qkv):
+        """A step from set `which` into the other one: O of each layer."""
+        old, new = self.sets[which], self.sets[1 - which]
+        fork = binding.attn_kv_fork(old["lengths"], source, old["table"], self.ring, old["state"], page_size=self.ps, pages=self.pages, table_out=new["table"], workspace=self.workspace[1])
+        binding.attn_kv_copy(self.both, fork.copies)
+        page = binding.attn_kv_pages(fork.lengths, self.one, new["table"], self.ring, fork.free_state, page_size=self.ps, tokens=self.R, lengths_out=new["lengths"],
+                                     free_state_out=new["state"])
+        shared = binding.attn_kv_shared_rows(new["table"], new["lengths"], self.offsets, page_size=self.ps)
+        out = []
+        for cache, x in zip(self.layers, qkv):
+            q, k, v = x.split((self.H, self.KH, self.KH), 1)
+            q, _, _ = binding.attn_qkv_prepare(q, k, v, positions=page.positions, cache=cache, slots=page.slots)
+            out.append(binding.attn_decode_shared(q, cache, new["table"], new["lengths"], self.offsets, shared, scale=self.d ** -0.5, workspace=self.workspace[0]))
+        return out, shared
+
+    def follow(self, source, qkv):
+        """The same on the host's side."""
+        for i, x in enumerate(qkv):
+            k, v = x[:, self.H:self.H + self.KH], x[:, self.H + self.KH:]
+            self.history[i] = [tuple(torch.cat([a, b[r:r + 1]]) for a, b in zip(self.history[i][s], (k, v))) for r, s in enumerate(source)]
+
+    def inputs(self, rng, g):
+        source = np.concatenate([p * self.beams + rng.integers(0, self.beams, self.beams) for p in range(self.R // self.beams)])
+        return source, [torch.randn(self.R, self.H + 2 * self.KH, self.d, generator=g, device="cuda").to(self.layers[0].dtype) for _ in self.layers]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,prompts,beams,H,KH,d,ps,wide", [("bf16", [77, 300], 4, 6, 2, 64, 16, 40), ("f16", [500, 16, 1], 16, 16, 8, 128, 32, 300),
+                                                               ("bf16", [1300, 900], 20, 32, 8, 128, 16, 100)])
+def test_a_search(dtype, prompts, beams, H, KH, d, ps, wide):
+    """Beams that branch, go on and end for some pages: every step's attention against each beam's own keys and values, kept apart; no page lost."""
+    rng, g = np.random.default_rng(1), torch.Generator("cuda").manual_seed(2)
+    b = Beams(prompts, beams, H, KH, d, ps, dtype, seed=3, wide=wide)
+    for i in range(2 * ps + 6):
+        source, qkv = b.inputs(rng, g)
+        out, shared = b.step(i % 2, up(source), qkv)
+        b.follow(source, qkv)
+        now = b.sets[1 - i % 2]
+        lengths = now["lengths"].tolist()
+        assert lengths == [prompts[r // beams] + i + 1 for r in range(b.R)]
+        assert all(s >= n // ps * ps for s, n in zip(shared.tolist(), prompts))
+        if i in (0, 1, ps - 1, ps, 2 * ps + 4, 2 * ps + 5):
+            for layer, o in enumerate(out):
+                check_shared(o, qkv[layer][:, :H], [[kv[j] for kv in b.history[layer]] for j in range(2)], d ** -0.5, lengths, dtype)
+        held = {p for r in range(b.R) for p in now["table"][r, :-(-lengths[r] // ps)].tolist()}
+        assert len(held) + int(now["state"][1]) == b.pages
+
+
+@pytest.mark.gpu
+def test_a_search_captured():
+    """Two steps captured into a graph, replayed with new sources and tokens, eager work and synchronizations between; every replay against a search that
+    makes the calls one by one."""
+    a, b = (Beams([1500, 700], 16, 32, 8, 128, 16, "bf16", seed=3, wide=110) for _ in range(2))
+    rng, g = np.random.default_rng(4), torch.Generator("cuda").manual_seed(5)
+    sources = [up([0] * a.R) for _ in range(2)]
+    first = [a.inputs(rng, g) for _ in range(2)]
+    qkv = [[x.clone() for x in f[1]] for f in first]
+    for s, f in zip(sources, first):
+        s.copy_(up(f[0]))
+    out = [b.step(i, sources[i], qkv[i])[0] for i in range(2)]      # (eagerly once, so that everything is loaded; on `a` it is the graph that steps)
+    kept = [{n: t.clone() for n, t in s.items()} for s in a.sets], a.ring.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = [a.step(i, sources[i], qkv[i])[0] for i in range(2)]
+    assert torch.equal(kept[1], a.ring)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for o, p in zip(outs, out) for x, y in zip(o, p))
+    for _ in range(12):
+        for i in range(2):
+            s, x = a.inputs(rng, g)
+            sources[i].copy_(up(s))
+            for t, y in zip(qkv[i], x):
+                t.copy_(y)
+        want = [b.step(i, sources[i], qkv[i])[0] for i in range(2)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for o, p in zip(outs, want) for x, y in zip(o, p))
+        assert all(torch.equal(x[n], y[n]) for x, y in zip(a.sets, b.sets) for n in ("lengths", "state")) and torch.equal(a.ring, b.ring)
+
+
+@pytest.mark.gpu
+def test_searches_on_streams_of_their_own():
+    """Two searches at once on two streams, each with its own workspaces, and calls that are given their stream: the results of one after the other."""
+    make = lambda i: Beams([1500, 700 + i], 16, 32, 8, 128, 16, "bf16", seed=3 + i, wide=110)
+    at_once, plain = [make(0), make(1)], [make(0), make(1)]
+    streams, rng, g = [torch.cuda.Stream(), torch.cuda.Stream()], np.random.default_rng(4), torch.Generator("cuda").manual_seed(5)
+    work = [[a.inputs(rng, g) for _ in range(6)] for a in at_once]
+    work = [[(up(s), x) for s, x in w] for w in work]
+    want = [[p.step(i % 2, *w[i])[0] for i in range(6)] for p, w in zip(plain, work)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for i in range(6):
+        for j in range(2):
+            with torch.cuda.stream(streams[j]):
+                got[j].append(at_once[j].step(i % 2, *work[j][i])[0])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for a, b in zip(got, want) for o, p in zip(a, b) for x, y in zip(o, p))
+    b, old = plain[0], plain[0].sets[0]
+    q, shared = queries(b.R, 32, 128, "bf16", seed=1), binding.attn_kv_shared_rows(old["table"], old["lengths"], b.offsets, page_size=16)
+    eager = binding.attn_decode_shared(q, b.layers[0], old["table"], old["lengths"], b.offsets, shared, scale=0.1, workspace=b.workspace[0])
+    fork = binding.attn_kv_fork(old["lengths"], work[0][0][0], old["table"], b.ring.clone(), old["state"], page_size=16, pages=b.pages)
+    torch.cuda.synchronize()
+    other = streams[0]
+    o = torch.zeros_like(eager)
+    torch.cuda.synchronize()
+    binding.attn_decode_shared(q, b.layers[0], old["table"], old["lengths"], b.offsets, shared, o, scale=0.1, workspace=b.workspace[0], stream=other)
+    again = binding.attn_kv_fork(old["lengths"], work[0][0][0], old["table"], b.ring.clone(), old["state"], page_size=16, pages=b.pages, stream=other)
+    s2 = binding.attn_kv_shared_rows(old["table"], old["lengths"], b.offsets, page_size=16, stream=other)
+    binding.attn_kv_copy(b.both, torch.full((3, 3), -1, dtype=torch.int32, device="cuda"), stream=other)
+    other.synchronize()
+    assert torch.equal(o, eager) and torch.equal(s2, shared) and torch.equal(again.lengths, fork.lengths) and torch.equal(again.copies, fork.copies)
+    assert torch.equal(again.free_state, fork.free_state)
+
+
+@pytest.mark.gpu
+def test_binding_refusals():
+    """What the calls refuse before they reach the library: types, shapes, sizes."""
+    case = fill_groups([(20, [3, 4])], [], 2, 64, 16, "f16", seed=1)
+    cache, table, lengths, offsets, shared, _ = case
+    lens, q = up(lengths), queries(2, 4, 64, "f16", seed=1)
+    binding.attn_decode_shared(q, cache, table, lens, offsets, shared, scale=0.1)
+    good = dict(q=q, cache=cache, table=table, lengths=lens, offsets=offsets, shared=shared)
+    for change in (dict(q=q.float()), dict(q=q[0]), dict(q=q.cpu()), dict(q=q[:, :, :32]), dict(table=table.long()), dict(table=table[:1]), dict(lengths=lens.long()), dict(lengths=lens[:1]),
+                   dict(offsets=offsets[:1]), dict(offsets=offsets.long()), dict(shared=shared.cpu()), dict(shared=shared.float()), dict(offsets=offsets.cpu())):
+        with pytest.raises(ValueError):
+            binding.attn_decode_shared(*{**good, **change}.values(), scale=0.1)
+    for kw in (dict(O=q[:1]), dict(O=q.double()), dict(workspace=torch.zeros(9))):
+        with pytest.raises(ValueError):
+            binding.attn_decode_shared(*good.values(), scale=0.1, **kw)
+    with pytest.raises(binding.SawattnError, match="smaller"):
+        binding.attn_decode_shared(*good.values(), scale=0.1, workspace=torch.zeros(64, device="cuda"))
+    ring, state, src = up(np.arange(9)), up([0, 9]), up([0, 1, 1])
+    call = lambda **kw: binding.attn_kv_fork(*[kw.pop(n, x) for n, x in (("lengths", lens), ("source", src), ("table", table), ("ring", ring), ("state", state))],
+                                             **{"page_size": 16, "pages": 9, **kw})
+    call()
+    for change in (dict(lengths=lens.long()), dict(source=src.float()), dict(table=table[:1]), dict(ring=ring.long()), dict(state=ring), dict(rows=lens), dict(table_out=table),
+                   dict(table_out=torch.zeros(3, table.shape[1] + 1, dtype=torch.int32, device="cuda")), dict(lengths_out=lens), dict(copies=src), dict(free_state_out=src),
+                   dict(workspace=torch.zeros(9)), dict(lengths=lens.cpu()), dict(source=src.cpu())):
+        with pytest.raises(ValueError):
+            call(**change)
+    with pytest.raises(binding.SawattnError, match="overlap"):
+        call(free_state_out=state)
+    with pytest.raises(binding.SawattnError, match="smaller"):
+        call(workspace=torch.zeros(4, device="cuda"))
+    for copies in (src.long(), up([1, 2, 3, 4]), src.cpu()):
+        with pytest.raises(ValueError):
+            binding.attn_kv_copy(cache, copies)
+    with pytest.raises(ValueError):
+        binding.KVLayers([])
+    with pytest.raises(ValueError):
+        binding.KVLayers([cache, binding.KVCache(cache.k[:, :1], cache.v[:, :1])])
+    for args in ((table, lens.long(), offsets), (table[:1], lens, offsets), (table, lens, offsets.long()), (table, lens.cpu(), offsets)):
+        with pytest.raises(ValueError):
+            binding.attn_kv_shared_rows(*args, page_size=16)
+    with pytest.raises(ValueError):
+        binding.attn_kv_shared_rows(table, lens, offsets, page_size=16, shared=lens)
+
+
+def test_built_kernels_have_no_scratch_memory(tmp_path):
+    import re
+    from .util import device_code, llvm_tool
+    notes = llvm_tool("llvm-readelf", "--notes", device_code(tmp_path))
+    found = dict(re.findall(r"\.name:\s+(_ZN7sawattn\d+(?:kv_(?:fork|fork_table|fork_free|fork_few|copy|shared_rows)|decode_shared|decode_shared_join)_kernel\S+)\s+"
+                            r"\.private_segment_fixed_size:\s+(\d+)", notes, re.S))
+    assert len(found) == 7 + 12 + 4 and set(found.values()) == {"0"}, found
+
+
+def test_built_wide_kernels_wait_for_what_they_send_to_lds(tmp_path):
+    """Between a direct load into LDS and the barrier behind which others read what it brought there is a wait for all of them."""
+    import re
+    from .util import device_listing, kernel_bodies
+    seen = 0
+    for kernel, body in kernel_bodies(device_listing(tmp_path)).items():
+        if not re.search(r"decode_shared_kernel<\d+, (true|false), 8>", kernel):
+            continue
+        flying, loads, barriers = False, 0, 0
+        for text, _ in body:
+            if text.startswith("global_load_lds_"):
+                flying, loads = True, loads + 1
+            elif re.match(r"s_waitcnt .*vmcnt\(0\)", text):
+                flying = False
+            elif text.startswith("s_barrier"):
+                assert not flying, kernel
+                barriers += 1
+        assert loads >= 8 and barriers >= 6, (kernel, loads, barriers)
+        seen += 1
+    assert seen == 4
