@@ -299,8 +299,7 @@ __global__ __launch_bounds__(kForkThreads) void kv_fork_few_kernel(ForkParams p)
 //
 // A row of a head is d elements side by side; of a copy there are heads * rows of them in each of K and V of each layer.  They are dealt out in
 // pieces of 64 rows (128 at d = 64), counted through all copies by a sum that every workgroup makes for itself (entries that are none cost nothing behind it).
-// Bound by memory: 121 pages of 64 rows and fewer, 8 heads of 128, in 16 layers, 242 MB read and written, 54 us, 4.5 TB/s (20 us of it at twice
-// that rate if all came from the Infinity Cache); loaded and stored cached 57.5.
+// Bound by memory: 121 pages of 64 rows and fewer, 8 heads of 128, in 16 layers, 242 MB read and written, 54 us, 4.5 TB/s; loaded and stored cached 57.5.
 constexpr int kCopyThreads = 256, kCopyLayers = 32, kCopyEach = SAWATTN_MOST_REQUESTS / kCopyThreads;
 constexpr int kCopyAhead = 4;      // 16-byte pieces of a thread on their way
 
@@ -378,7 +377,8 @@ __global__ __launch_bounds__(kCopyThreads) void kv_copy_kernel(CopyParams p) {
 
 // ---- common rows
 //
-// A workgroup to a group; a thread to a table column, of which it looks at all requests' entries, sixteen on their way at a time.
+// A workgroup to a group; a thread to a table column, of which it looks at all requests' entries (or a share of them, where there are fewer columns than threads),
+// sixteen on their way at a time.  8 requests of 250 pages 3.9 us, 40 groups of 25 of up to 1024 pages 7, one of 256 requests of 260 pages 13.
 constexpr int kCommonThreads = 1024, kCommonAhead = 16;
 
 __global__ __launch_bounds__(kCommonThreads) void kv_shared_rows_kernel(const int* lengths, const int* table, long long stride, int max_pages, int shift,
@@ -403,12 +403,14 @@ __global__ __launch_bounds__(kCommonThreads) void kv_shared_rows_kernel(const in
     __syncthreads();
     const int n = count;
     const int pages = n ? min(least >> shift, max_pages) : 0;
-    for (int j0 = 0; j0 < pages; j0 += kCommonThreads) {
-        const int j = j0 + tid;
+    int across = kCommonThreads;      // columns at a time; the threads that are left over take other requests
+    while (across > 64 && across / 2 >= pages) across /= 2;
+    for (int j0 = 0; j0 < pages; j0 += across) {
+        const int j = j0 + (tid & (across - 1));
         if (j < pages) {
             const int page = table[there[0] * stride + j];
             bool same = true;
-            for (int i0 = 1; i0 < n; i0 += kCommonAhead) {
+            for (int i0 = 1 + tid / across * kCommonAhead; i0 < n; i0 += kCommonAhead * (kCommonThreads / across)) {
                 int other[kCommonAhead];
 #pragma unroll
                 for (int i = 0; i < kCommonAhead; ++i) other[i] = table[there[min(i0 + i, n - 1)] * stride + j];
@@ -418,7 +420,7 @@ __global__ __launch_bounds__(kCommonThreads) void kv_shared_rows_kernel(const in
             if (!same) atomicMin(&differ, j);
         }
         __syncthreads();
-        if (differ < j0 + kCommonThreads) break;      // (uniform: nobody changes it before the next barrier)
+        if (differ < j0 + across) break;      // (uniform: nobody changes it before the next barrier)
         __syncthreads();
     }
     if (tid == 0) shared[g] = min(differ, pages) << shift;

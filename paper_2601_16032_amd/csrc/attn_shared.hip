@@ -17,11 +17,11 @@
 //
 // Products run on 16x16x32 MFMAs, transposed: S^T = K Q^T, O^T = V^T P^T.  Up to 32 columns (RowsState) and tails: rows from memory straight into the operands' registers.  More:
 // tiles of 64 rows through LDS that the four wavefronts share, 32 columns each (WideState).  NB is 1, 2 or 8, by the columns that the groups have on average: with
-// 2 for all of them, 64 requests of 4 heads to a key head behind 8192 rows take 41 us, with 8 31; 256 behind 32768 242 and 200.
+// 2 for all of them, 256 requests of 4 heads to a key head behind 32768 rows take 242 us, with 8 200 (64 behind 8192 31 and 30; tails left out).
 //
 // The probabilities enter the second product as sums of two 16-bit numbers (SharedPieces), 16 bits of them: one would be off by as much as the
-// rounding of O to 16 bits, three, as in attn_decode, would take a third more of the matrix cores.  The larger cases run at 1.0 PFLOP/s of MFMAs, 45 % of the rate at 2.1 GHz, which
-// is the clock that the chip then holds; MFMA phases have precedence (210 -> 200 us for 256 requests behind 32768 rows).
+// rounding of O to 16 bits, three, as in attn_decode, would take a third more of the matrix cores.  256 requests behind 32768 rows, with their tails, run at 0.88 PFLOP/s of MFMAs, 40 % of the rate at 2.1 GHz,
+// which is the clock that the chip then holds; MFMA phases have precedence (210 -> 200 us without the tails).
 namespace sawattn {
 
 constexpr int kSharedThreads = 64 * kDecodeWaves;
@@ -89,9 +89,8 @@ struct RowsPages {      // of the two halves of a tile
     __device__ __forceinline__ bool bad(const DecodeParams& p, int i) const { return (unsigned)half[i] >= (unsigned)p.pages; }
 };
 
-// A wavefront's part of a tail unit, or of a prefix unit of up to 32 columns: tiles of 32 rows in registers, the next one's loads behind the product that uses them up (a second set
-// of registers, or K by way of LDS in whole rows, gave nothing: the loops are entered once or twice in most calls, and what counts is how much
-// code there is to fetch; 64 requests with tails up to 1000 24.5, 26 and 22.4 us).  V is read once and past the caches; K's rows come in four loads of 64
+// A wavefront's part of a tail unit, or of a prefix unit of up to 32 columns: tiles of 32 rows in registers, the next one's loads behind the product that uses them up.  Tails alone, 64
+// requests of up to 1000 rows and 256 of up to 2000: 22.4 and 87 us; by workgroups, with tiles in LDS, 18.6 and 96; with a second set of registers 64 take 24.5.  V is read once and past the caches; K's rows come in four loads of 64
 // bytes each, of which the caches join two (non-temporal: 10 % longer).
 template <int D, bool BF16, int NB>
 struct RowsState {
@@ -997,7 +996,8 @@ int launch_shared(const SharedParams& p, int grid, hipStream_t stream) {
     if (rc != SAWATTN_OK) return rc;
     const int rows = p.d.R * p.H;
     constexpr int kAcross = D / 4, kRows4 = kSharedJoinThreads / (4 * kAcross), kRows1 = kSharedJoinThreads / kAcross;
-    if (rows <= 2048) hipLaunchKernelGGL((decode_shared_join_kernel<D, 4>), dim3((rows + kRows4 - 1) / kRows4), dim3(kSharedJoinThreads), 0, stream, p, 16 * blocks, grid);
+    // (2080 rows of 5 parts 7.9 us with 4, 8.7 with 1; 8192 of 4 17 and 11)
+    if (rows <= 4096) hipLaunchKernelGGL((decode_shared_join_kernel<D, 4>), dim3((rows + kRows4 - 1) / kRows4), dim3(kSharedJoinThreads), 0, stream, p, 16 * blocks, grid);
     else hipLaunchKernelGGL((decode_shared_join_kernel<D, 1>), dim3((rows + kRows1 - 1) / kRows1), dim3(kSharedJoinThreads), 0, stream, p, 16 * blocks, grid);
     return launched("attn_decode_shared");
 }

@@ -1,4 +1,4 @@
-"""The paper's cache studies as sweeps over the attention kernel, and decoding steps over a paged cache (one GPU).
+"""The paper's cache studies as sweeps over the attention kernel, and decoding steps and searches over a paged cache (one GPU).
 
 Each study is a list of points (shape, launch variant, scan order).  A point is run as
 `--warmup` untimed plus `--launches` timed launches of the HIP kernel through the C ABI (after `--settle-ms`
@@ -23,6 +23,8 @@ Studies
   steps     Decoding behind the prompt: one step (attn_kv_pages, attn_qkv_prepare, attn_decode) of R requests whose caches hold
             `length` rows in pages of 64 in any order, ungrouped and grouped heads; each of the three timed for itself, with the bytes
             per second that attn_decode reads of the cache.
+  beams     A step of a search: `prompts` groups of `beams` requests that have `common` rows of their prompt in the same pages and `own` rows each behind them
+            (attn_kv_fork, attn_kv_copy, attn_kv_shared_rows, attn_decode_shared, and attn_decode on the same tables beside it); each timed for itself.
 
 A point without a variant runs what attn_fwd runs (launch left open); a variant pins the persistent launch unless
 it names the other.  seqlen and batch are about rounds that share an L2 and pin the persistent launch, which attn_fwd
@@ -97,6 +99,10 @@ def study_points(study: str):
         for (H, KH, d) in ((8, 8, 64), (32, 32, 128), (32, 8, 128)):
             for (R, length) in ((1, 255), (1, 16384), (1, 131071), (8, 4096), (64, 2048), (256, 512), (16, 32768)):
                 pts.append({"R": R, "length": length, "H": H, "KH": KH, "d": d})
+    elif study == "beams":
+        for (H, KH, d) in ((8, 8, 64), (32, 8, 128)):
+            for (prompts, beams, common, own) in ((1, 4, 1024, 40), (1, 8, 8192, 200), (16, 4, 2048, 100), (8, 16, 4096, 200), (1, 64, 8192, 500), (1, 256, 16384, 300)):
+                pts.append({"prompts": prompts, "beams": beams, "common": common, "own": own, "H": H, "KH": KH, "d": d})
     else:
         raise SystemExit(f"unknown study {study!r}")
     return pts
@@ -143,11 +149,47 @@ def decode_step(pt, dtype="bf16", seed=0):
     ], held_by
 
 
+def search_step(pt, dtype="bf16", seed=0):
+    """The calls of one step of a search that work on shared pages, of a point of the study `beams`: [(operator, call)], to be called in order, and what they work
+    on.  The step can be repeated: what a fork writes lies beside what it reads, and the pages it gives back are the same ones each time."""
+    import torch
+    from . import binding as sa
+    prompts, beams, common, own, H, KH, d = (pt[n] for n in ("prompts", "beams", "common", "own", "H", "KH", "d"))
+    dt, ps, R = {"f16": torch.float16, "bf16": torch.bfloat16}[dtype], STEP_PAGE_SIZE, prompts * beams
+    g = torch.Generator("cuda").manual_seed(seed)
+    i32 = {"dtype": torch.int32, "device": "cuda"}
+    whole, held = common // ps, -(-(common + own) // ps)
+    used = prompts * whole + R * (held - whole)
+    pages = used + R
+    order = torch.randperm(pages, generator=g, device="cuda").int()
+    table = torch.empty(prompts, beams, held, **i32)
+    table[:, :, :whole] = order[:prompts * whole].view(prompts, 1, whole)
+    table[:, :, whole:] = order[prompts * whole:used].view(prompts, beams, held - whole)
+    table = table.view(R, held)
+    ring, state = order.roll(-used), torch.tensor([0, R], **i32)
+    cache = sa.KVCache(*(torch.randn(pages, KH, ps, d, generator=g, device="cuda", dtype=dt) for _ in range(2)))
+    lengths, offsets = torch.full((R,), common + own, **i32), torch.arange(prompts + 1, **i32) * beams
+    source = (torch.arange(R, device="cuda") // beams * beams + torch.randint(0, beams, (R,), generator=g, device="cuda")).int()
+    q = torch.randn(R, H, d, generator=g, device="cuda", dtype=dt)
+    fork = sa.ForkStep(torch.zeros_like(table), torch.zeros_like(lengths), torch.zeros(R, 3, **i32), torch.zeros(2, **i32))
+    workspaces = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (
+        sa.attn_kv_fork_workspace_bytes(R, R, pages), sa.attn_decode_shared_workspace_bytes(R, H, prompts, cache, held), sa.attn_decode_workspace_bytes(R, H, cache, held))]
+    shared, outs, scale = torch.zeros(prompts, **i32), [torch.empty_like(q) for _ in range(2)], 1.0 / math.sqrt(d)
+    return [
+        ("attn_kv_fork", lambda: sa.attn_kv_fork(lengths, source, table, ring, state, page_size=ps, pages=pages, table_out=fork.table, lengths_out=fork.lengths,
+                                                 copies=fork.copies, free_state_out=fork.free_state, workspace=workspaces[0])),
+        ("attn_kv_copy", lambda: sa.attn_kv_copy(cache, fork.copies)),
+        ("attn_kv_shared_rows", lambda: sa.attn_kv_shared_rows(fork.table, fork.lengths, offsets, page_size=ps, shared=shared)),
+        ("attn_decode_shared", lambda: sa.attn_decode_shared(q, cache, fork.table, fork.lengths, offsets, shared, outs[0], scale=scale, workspace=workspaces[1])),
+        ("attn_decode", lambda: sa.attn_decode(q, cache, fork.table, fork.lengths, outs[1], scale=scale, workspace=workspaces[2])),
+    ], {"cache": cache, "table": table, "source": source, "fork": fork, "shared": shared, "q": q, "o": outs[0], "o_apart": outs[1]}
+
+
 def run_steps(pts, chosen, args):
     import torch
     for i in chosen:
         pt = pts[i]
-        calls, _ = decode_step(pt, seed=1234 + i)
+        calls, _ = (search_step if "beams" in pt else decode_step)(pt, seed=1234 + i)
         out = {}
         for name, call in calls:
             for _ in range(args.warmup + 1):
@@ -160,8 +202,11 @@ def run_steps(pts, chosen, args):
                 ev[k + 1].record()
             torch.cuda.synchronize()
             out[name + "_us"] = round(sorted(ev[k].elapsed_time(ev[k + 1]) / 8e-3 for k in range(args.launches))[args.launches // 2], 2)
-        read = 4.0 * pt["R"] * (pt["length"] + 1) * pt["KH"] * pt["d"]
-        print(json.dumps({"study": "steps", "point": i, **pt, **out, "cache_gb_per_s": round(read / out["attn_decode_us"] / 1e3, 1)}), flush=True)
+        if "beams" in pt:
+            print(json.dumps({"study": "beams", "point": i, **pt, **out}), flush=True)
+        else:
+            read = 4.0 * pt["R"] * (pt["length"] + 1) * pt["KH"] * pt["d"]
+            print(json.dumps({"study": "steps", "point": i, **pt, **out, "cache_gb_per_s": round(read / out["attn_decode_us"] / 1e3, 1)}), flush=True)
         del calls
         torch.cuda.empty_cache()
     return 0
@@ -187,7 +232,7 @@ def model(pt, info):
 
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
-    ap.add_argument("--study", required=True, choices=["seqlen", "resident", "decode", "launch", "batch", "heads", "steps"])
+    ap.add_argument("--study", required=True, choices=["seqlen", "resident", "decode", "launch", "batch", "heads", "steps", "beams"])
     ap.add_argument("--points", default="", help="comma-separated point indices or a:b ranges (default: all)")
     ap.add_argument("--launches", type=int, default=3)
     ap.add_argument("--warmup", type=int, default=1)
@@ -217,7 +262,7 @@ def main(argv=None):
     if not torch.cuda.is_available():
         raise SystemExit("sweeps need a GPU (there is no CPU path)")
     sa.lib()
-    if args.study == "steps":
+    if args.study in ("steps", "beams"):
         return run_steps(pts, chosen, args)
     stream = torch.cuda.current_stream()
     cache = {}

@@ -877,3 +877,32 @@ def test_built_wide_kernels_wait_for_what_they_send_to_lds(tmp_path):
         assert loads >= 8 and barriers >= 6, (kernel, loads, barriers)
         seen += 1
     assert seen == 4
+
+
+def test_beams_study_lists_its_points(capsys):
+    from paper_2601_16032_amd import sweeps
+    assert sweeps.main(["--study", "beams", "--list"]) == 0
+    assert len(capsys.readouterr().out.splitlines()) == len(sweeps.study_points("beams")) == 12
+
+
+@pytest.mark.gpu
+def test_beams_study_runs(capsys):
+    """Points of the study `beams`: every operator timed, and the step right, repeated too."""
+    import json
+    from paper_2601_16032_amd import sweeps
+    assert sweeps.main(["--study", "beams", "--points", "0,8", "--launches", "2"]) == 0
+    lines = [json.loads(x) for x in capsys.readouterr().out.splitlines() if x.startswith("{")]
+    names = ("attn_kv_fork", "attn_kv_copy", "attn_kv_shared_rows", "attn_decode_shared", "attn_decode")
+    assert [x["point"] for x in lines] == [0, 8] and all(x[n + "_us"] > 0 for x in lines for n in names)
+    calls, held = sweeps.search_step({"prompts": 3, "beams": 20, "common": 1000, "own": 77, "H": 16, "KH": 8, "d": 128}, dtype="f16", seed=3)
+    for _ in range(2):
+        for _, call in calls:
+            call()
+    torch.cuda.synchronize()
+    cache, fork = held["cache"], held["fork"]
+    assert fork.lengths.tolist() == [1077] * 60 and held["shared"].tolist() == [960] * 3
+    keys = [[x[t.long()].transpose(1, 2).reshape(-1, 8, 128)[:1077] for t in fork.table] for x in (cache.k, cache.v)]
+    parents = [[x[held["table"][int(s)].long()].transpose(1, 2).reshape(-1, 8, 128)[:1077] for s in held["source"]] for x in (cache.k, cache.v)]
+    assert all(torch.equal(a, b) for side, kept in zip(keys, parents) for a, b in zip(side, kept))
+    check_shared(held["o"], held["q"], keys, 128 ** -0.5, [1077] * 60, "f16")
+    check_shared(held["o_apart"], held["q"], keys, 128 ** -0.5, [1077] * 60, "f16")
