@@ -449,7 +449,8 @@ int attn_decode_workspace_bytes(const sawattn_kv_cache* cache, int R, int H, int
  *   - every other one takes a fresh page from the front of the free list, in the order of the requests, and copies[r] says what has to be copied
  *     into it.  Where no page is left the request gets nothing: its length becomes 0 and copies[r] = (page, -1, rows).
  * Every page that a request of the old batch holds and none of the new one does goes behind the last free one, in the order of their numbers (to be
- * taken from the next call on).  A request of the old batch that no new one names has ended.
+ * taken from the next call on).  A request of the old batch that no new one names has ended.  The copies are due before a row is written to a page and before the
+ * next call that takes pages: what has to be copied from may be written on by the request that took it over, or be among the pages given back.
  *
  *   lengths         device, read: int32 [R], 1 <= R <= SAWATTN_MOST_REQUESTS.  Below 0 they count as 0, above max_pages*page_size as that.
  *   source          device, read: int32 [N], 1 <= N <= SAWATTN_MOST_REQUESTS; outside 0 .. R - 1: an empty request
@@ -459,7 +460,7 @@ int attn_decode_workspace_bytes(const sawattn_kv_cache* cache, int R, int H, int
  *   table_out       device, written: int32 [N] rows, likewise; entries behind a request's pages are left as they are
  *   max_pages, page_size  as in attn_kv_pages (R*max_pages and N*max_pages below 2^31)
  *   pages           of the cache, >= 1
- *   free_pages      device, read and written: int32 [ring], as in attn_kv_pages
+ *   free_pages      device, read and written: int32 [ring], as in attn_kv_pages (pages given back for which it has no room are lost)
  *   free_state      device, read: int32 [2]
  *   lengths_out     device, written: int32 [N]
  *   copies          device, written: int32 [N][3] = (page to copy from, page to copy to, rows), (-1, -1, 0) where there is nothing to copy

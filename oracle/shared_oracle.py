@@ -41,7 +41,7 @@ def kv_fork(lengths, source, rows, table, free, state, page_size, pages, table_o
     back = sorted(p for p in held - kept if 0 <= p < pages)
     for i, p in enumerate(back[:F - available]):
         ring[(first + available + i) % F] = p
-    return out, out_len, copies, ring, [(first + used) % F, min(available - used + len(back), F)]
+    return out, out_len, copies, ring, [(first + used) % F, available - used + min(len(back), F - available)]
 
 
 def shared_rows(table, lengths, offsets, page_size):

@@ -14,7 +14,8 @@ namespace sawattn {
 
 constexpr int kForkThreads = 1024, kForkEach = SAWATTN_MOST_REQUESTS / kForkThreads;      // requests of a thread at most
 constexpr int kForkTableThreads = 256, kForkRow = 4 * kForkTableThreads;                   // table entries of a workgroup
-constexpr int kForkPages = 16 * kForkThreads;                                              // pages of a workgroup, 16 marks of a thread
+constexpr int kForkPages = 16 * kForkThreads, kForkFreeGrid = 256;                         // pages of a workgroup at a time, 16 marks of a thread; workgroups at most (every
+                                                                                           // one reads the marks in front of its own)
 constexpr int kForkFewRequests = kForkThreads, kForkFewPages = 1 << 17, kForkFewEntries = 1 << 14;      // of a call that one workgroup does all of, at most
 
 struct ForkParams {
@@ -209,38 +210,46 @@ __global__ __launch_bounds__(kForkTableThreads) void kv_fork_table_kernel(ForkPa
     }
 }
 
-// Pages that were held and are no longer, by their numbers, behind the last one in the ring.  Every workgroup counts those in front of its own.
-__global__ __launch_bounds__(kForkThreads) void kv_fork_free_kernel(ForkParams p) {
+// Pages that were held and are no longer, by their numbers, behind the last one in the ring.  A workgroup takes `each` times kForkPages and counts those in front of its own.
+__global__ __launch_bounds__(kForkThreads) void kv_fork_free_kernel(ForkParams p, int each) {
     __shared__ int of_wave[2][kForkThreads / 64];
     const int tid = threadIdx.x;
-    auto freed = [&](int word) {      // one bit to a byte
+    auto freed = [&](unsigned word) {      // one bit to a byte
         u4 m = {0, 0, 0, 0};
-        if (word < p.mark_words) m = p.held[word] & ~p.kept[word];
+        if (word < (unsigned)p.mark_words) m = p.held[word] & ~p.kept[word];
         return m;
     };
     auto count = [](u4 m) { return __popc(m[0]) + __popc(m[1]) + __popc(m[2]) + __popc(m[3]); };
-    const u4 mine = freed(blockIdx.x * kForkThreads + tid);
+    const unsigned chunk0 = blockIdx.x * each;
+    u4 mine = freed(chunk0 * kForkThreads + tid);
     const int2 taken = *p.taken;
     const ForkRing ring(p);
     int in_front = 0;
 #pragma unroll 4
-    for (unsigned c = 0; c < blockIdx.x; ++c) in_front += count(freed(c * kForkThreads + tid));
-    int front, own;
-    block_before(in_front, of_wave[0], front);
-    int before = front + block_before(count(mine), of_wave[1], own);
+    for (unsigned c = 0; c < chunk0; ++c) in_front += count(freed(c * kForkThreads + tid));
+    int all;      // in front of the chunk
+    block_before(in_front, of_wave[0], all);
     const int room = p.ring_size - taken.y;      // (there is room for all of them if the ring has a place for every page)
-    if (count(mine))
+    for (unsigned chunk = chunk0;;) {
+        int own;
+        int before = all + block_before(count(mine), of_wave[1], own);
+        if (count(mine))
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
+            for (int w = 0; w < 4; ++w)
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-                if (mine[w] >> (8 * b) & 1) {
-                    if (before < room) p.ring[ring.at((unsigned long long)taken.y + (unsigned)before)] = (blockIdx.x * kForkThreads + tid) * 16 + w * 4 + b;
-                    ++before;
-                }
+                for (int b = 0; b < 4; ++b)
+                    if (mine[w] >> (8 * b) & 1) {
+                        if (before < room) p.ring[ring.at((unsigned long long)taken.y + (unsigned)before)] = (int)((chunk * kForkThreads + tid) * 16 + w * 4 + b);
+                        ++before;
+                    }
+        all += own;
+        if (++chunk == chunk0 + each) break;
+        mine = freed(chunk * kForkThreads + tid);
+        __syncthreads();      // of_wave has been read
+    }
     if (blockIdx.x == gridDim.x - 1 && tid == 0) {
         p.state_out[0] = (int)ring.at((unsigned)taken.x);
-        p.state_out[1] = (int)min((long long)taken.y - taken.x + front + own, (long long)p.ring_size);
+        p.state_out[1] = taken.y - taken.x + min(all, room);
     }
 }
 
@@ -291,7 +300,7 @@ __global__ __launch_bounds__(kForkThreads) void kv_fork_few_kernel(ForkParams p)
     }
     if (tid == 0) {
         p.state_out[0] = (int)ring.at((unsigned)taken);
-        p.state_out[1] = (int)min((long long)ring.available - taken + all, (long long)p.ring_size);
+        p.state_out[1] = ring.available - taken + min(all, room);
     }
 }
 
@@ -503,7 +512,8 @@ int attn_kv_fork(const int32_t* lengths, int R, const int32_t* source, const int
     hipLaunchKernelGGL(kv_fork_table_kernel, dim3((R + N) * parts), dim3(kForkTableThreads), 0, stream, p, parts);      // (below 2^22 + 2^13)
     status = launched("attn_kv_fork");
     if (status != SAWATTN_OK) return status;
-    hipLaunchKernelGGL(kv_fork_free_kernel, dim3((unsigned)(((long long)pages + kForkPages - 1) / kForkPages)), dim3(kForkThreads), 0, stream, p);
+    const int chunks = (int)(((long long)pages + kForkPages - 1) / kForkPages), each = (chunks + kForkFreeGrid - 1) / kForkFreeGrid;
+    hipLaunchKernelGGL(kv_fork_free_kernel, dim3((chunks + each - 1) / each), dim3(kForkThreads), 0, stream, p, each);
     return launched("attn_kv_fork");
 }
 

@@ -241,7 +241,7 @@ def test_fork_everything_ends():
 def test_fork_many_pages():
     """More pages than one workgroup looks at, in any order, those given back among all of them."""
     rng = np.random.default_rng(11)
-    for pages in (16384, 16385, 50000, 131072 + 7):
+    for pages in (16384, 16385, 50000, 131072, 131072 + 7, 256 * 16384 + 5, 3 * 256 * 16384 - 7):
         lengths = np.array([16 * 900, 16 * 800 + 3, 16 * 700])
         table = np.zeros((3, 901), dtype=np.int64)
         ids = rng.permutation(pages)
@@ -251,6 +251,18 @@ def test_fork_many_pages():
         ring[:50] = ids[3000:3050]
         check_fork(lengths, np.array([1, 1, 0]), np.array([16 * 500 + 1, 16 * 800 + 2, 16 * 300]), table, ring, [0, 50], 16, pages)
         check_fork(lengths, np.array([-1]), None, table, ring, [0, 50], 16, pages)
+
+
+@pytest.mark.gpu
+def test_fork_into_a_ring_too_small():
+    """Pages given back that the ring has no room for are lost, and none of those in use is counted as free in their place."""
+    rng = np.random.default_rng(12)
+    for wide in (8, 800):
+        lengths, table = np.full(30, 16 * wide - 3), np.arange(30 * wide).reshape(30, wide)
+        ring = np.arange(30 * wide, 30 * wide + 40)
+        for state in ([0, 32], [37, 40], [20, 0], [39, 39]):
+            check_fork(lengths, rng.integers(0, 30, 12), rng.integers(1, 16 * wide, 12), table, ring, state, 16, 31 * wide + 40)
+            check_fork(lengths, np.array([3, 3]), np.array([17, 18]), table, ring, state, 16, 31 * wide + 40)
 
 
 @pytest.mark.gpu
@@ -498,7 +510,8 @@ def test_decode_shared_outputs_and_scales(dtype, out, scale):
 @pytest.mark.parametrize("groups,KH,G,d", [([(16, [0] * 2)], 1, 1, 64), ([(200, [1] * 100)], 2, 4, 128), ([(4096, [100] * 70)], 1, 8, 64), ([(30000, [5, 1000, 77, 0])], 2, 4, 128),
                                           ([(64 * i, [i, 2 * i, 0]) for i in range(1, 60)], 1, 2, 64), ([(100000, [3, 3])], 1, 1, 128), ([(33, [2])] * 300, 1, 3, 64),
                                           ([(160, [1, 2])] * 1500, 1, 1, 64), ([(0, [20] * 4)] * 3, 8, 4, 128), ([(700, [1] * 5)] * 40, 8, 7, 128),
-                                          ([(64, [1] * 64)] * 64, 1, 1, 128), ([(0, [1])] * 4096, 1, 1, 64), ([(32, [5, 9] * 20)] * 3, 2, 33, 128), ([(1500, [700] * 90)], 1, 2, 64)])
+                                          ([(64, [1] * 64)] * 64, 1, 1, 128), ([(0, [1])] * 4096, 1, 1, 64), ([(32, [5, 9] * 20)] * 3, 2, 33, 128), ([(1500, [700] * 90)], 1, 2, 64),
+                                          ([(0, [1])] * 4094 + [(48, [1, 2])], 1, 40, 128)])
 def test_decode_shared_sizes(groups, KH, G, d):
     """One step to a workgroup and many, one unit and thousands, groups that a unit holds and groups of many units."""
     case = fill_groups(groups, [], KH, d, 16, "bf16", seed=len(groups))
