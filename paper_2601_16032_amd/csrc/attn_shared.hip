@@ -11,7 +11,7 @@
 // Who does what.  The steps (128 rows) of all prefix units, one behind the other, are dealt out evenly over workgroups, and the tiles (32 rows) of all tail
 // units, the other way round, over wavefronts.  With much to do every workgroup takes its share of both, and of the two workgroups of a compute unit
 // one begins with prefixes and one with tails, so that one computes while the other waits for memory (256 requests behind 32768 rows, 32 + 2 x 8 heads of 128,
-// tails up to 2000: 250 us; prefixes alone 190, tails alone 87).  With little to do a workgroup takes one kind only, where that ends sooner: what
+// tails up to 2000: 250 us; prefixes alone 190, tails alone 105).  With little to do a workgroup takes one kind only, where that ends sooner: what
 // counts then are the steps from one address to the next, a microsecond each.  Of each unit that a workgroup ends, begins or goes on with it leaves
 // (m, l, o) in the workspace, and a second kernel joins for every row of O what belongs to it.
 //
@@ -22,6 +22,8 @@
 // The probabilities enter the second product as sums of two 16-bit numbers (SharedPieces), 16 bits of them: one would be off by as much as the
 // rounding of O to 16 bits, three, as in attn_decode, would take a third more of the matrix cores.  256 requests behind 32768 rows, with their tails, run at 0.88 PFLOP/s of MFMAs, 40 % of the rate at 2.1 GHz,
 // which is the clock that the chip then holds; MFMA phases have precedence (210 -> 200 us without the tails).
+// Without their tails they take 190 us, 1.08 PFLOP/s; a large product reaches 1.28.  A pipeline in which the exponentials of 32 rows stand between the MFMAs of the rows before and
+// behind them was no faster (209 us; 178 with nothing but its MFMAs and what feeds them).
 namespace sawattn {
 
 constexpr int kSharedThreads = 64 * kDecodeWaves;
@@ -90,7 +92,7 @@ struct RowsPages {      // of the two halves of a tile
 };
 
 // A wavefront's part of a tail unit, or of a prefix unit of up to 32 columns: tiles of 32 rows in registers, the next one's loads behind the product that uses them up.  Tails alone, 64
-// requests of up to 1000 rows and 256 of up to 2000: 22.4 and 87 us; by workgroups, with tiles in LDS, 18.6 and 96; with a second set of registers 64 take 24.5.  V is read once and past the caches; K's rows come in four loads of 64
+// requests of up to 1000 rows and 256 of up to 2000: 22.4 and 87 us (read from the Infinity Cache in part); by workgroups, with tiles in LDS, 18.6 and 96; with a second set of registers 64 take 24.5.  V is read once and past the caches; K's rows come in four loads of 64
 // bytes each, of which the caches join two (non-temporal: 10 % longer).
 template <int D, bool BF16, int NB>
 struct RowsState {
