@@ -3,7 +3,7 @@
 //   s_j = scale q . k_j,  o = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m);  over two sets of rows with (m1, l1, o1) and (m2, l2, o2), o = sum p v:
 //   m = max(m1, m2),  O = (exp(m1 - m) o1 + exp(m2 - m) o2) / (exp(m1 - m) l1 + exp(m2 - m) l2)
 //
-// A prefix unit is a group's common rows in one key/value head, with up to 16 NB of the query heads that look at them (its columns: all query
+// A prefix unit is a group's common rows in one key/value head, with up to 128 of the query heads that look at them (its columns: all query
 // heads of that key head of all requests of the group, one request's behind the other's); a tail unit is the rows behind them of one request, with up
 // to 16 of its query heads, as in attn_decode.  Tails are bound by memory.  A prefix is read once for a unit's columns, 6 d operations of the matrix cores
 // (below) for each of them per 4 d bytes: from 64 columns on it is the matrix cores' and the vector units' time that counts.
@@ -16,8 +16,9 @@
 // (m, l, o) in the workspace, and a second kernel joins for every row of O what belongs to it.
 //
 // Products run on 16x16x32 MFMAs, transposed: S^T = K Q^T, O^T = V^T P^T.  Up to 32 columns (RowsState) and tails: rows from memory straight into the operands' registers.  More:
-// tiles of 64 rows through LDS that the four wavefronts share, 32 columns each (WideState).  NB is 1, 2 or 8, by the columns that the groups have on average: with
-// 2 for all of them, 256 requests of 4 heads to a key head behind 32768 rows take 242 us, with 8 200 (64 behind 8192 31 and 30; tails left out).
+// tiles of 64 rows through LDS that the four wavefronts share, 32 columns each (WideState); 32 columns at a time, 256 requests of 4 heads to a key head behind 32768 rows take 242 us
+// instead of 190 (64 behind 8192 31 and 30; tails left out).  Which it is goes by the unit, so groups of any sizes stand in one call: 256 requests behind 16384 rows and 256 of their own 311 us, 522 with
+// units as wide as the groups' mean; kernels of their own for calls of 16 or 32 columns at most gain 1 to 2 %.
 //
 // The probabilities enter the second product as sums of two 16-bit numbers (SharedPieces), 16 bits of them: one would be off by as much as the
 // rounding of O to 16 bits, three, as in attn_decode, would take a third more of the matrix cores.  256 requests behind 32768 rows, with their tails, run at 0.88 PFLOP/s of MFMAs, 40 % of the rate at 2.1 GHz,
@@ -28,7 +29,7 @@ namespace sawattn {
 
 constexpr int kSharedThreads = 64 * kDecodeWaves;
 constexpr int kSharedGrid = 512;      // workgroups: two to a compute unit
-constexpr int kSharedMostColumns = 128;
+constexpr int kSharedColumns = 128;   // of a prefix unit at most
 // Bytes of K and V, every request's counted, with the tables full, up to which they are read request by request all the same, by attn_decode's kernels; more where these
 // need one launch.  The two here take 12 us at least.  32 + 2 x 8 heads of 128, requests x rows in common + own: 4 x 2000 + 100, 35 MB: 14.2 us, attn_decode 12.1; 8 x 2000 + 100, 69 MB: 14.8
 // and 16.9; in one launch (the caches serve most of what is read again) 64 x 500 + 100, 159 MB: 20.7 and 11.3.
@@ -42,7 +43,7 @@ struct SharedParams {
     float c;                  // |scale| * log2(e), 1e-30 at least: the factor of the scores ...
     int negative;             // ... and whether the queries change sign
     // workspace
-    float* prefix_parts;      // [2 * grid][columns of a unit][D]
+    float* prefix_parts;      // [2 * grid][kSharedColumns][D]
     f2* prefix_sums;
     float* tail_parts;        // [2 * wavefronts of the grid][heads_kept][D]
     f2* tail_sums;
@@ -502,13 +503,11 @@ struct SharedStart {      // of a workgroup's share, found by one of its threads
     int item, inside;
 };
 
-template <int D, bool BF16, int NB>
+template <int D, bool BF16>
 __global__ __launch_bounds__(kSharedThreads, 2) void decode_shared_kernel(SharedParams p) {
-    constexpr int kPitch = D + 4, kArea = kDecodeHeads * kPitch * 4, kColumns = 16 * NB;
-    constexpr bool WIDE = NB > 2;
-    constexpr int kBuffer = 2 * WideLane<D>::kTile;
-    static_assert(!WIDE || kColumns == 128, "a wavefront has 32 columns");
-    __shared__ __align__(16) char memory[WIDE ? std::max(kDecodeWaves * kArea, 2 * kBuffer) : kDecodeWaves * kArea];
+    constexpr int kPitch = D + 4, kArea = kDecodeHeads * kPitch * 4, kColumns = kSharedColumns, kBuffer = 2 * WideLane<D>::kTile;
+    static_assert(kColumns == 32 * kDecodeWaves, "a wavefront has 32 columns");
+    __shared__ __align__(16) char memory[std::max(kDecodeWaves * kArea, 2 * kBuffer)];
     auto& area = *reinterpret_cast<char (*)[kDecodeWaves][kArea]>(memory);      // a wavefront's own
     __shared__ float m_of[kDecodeWaves][kDecodeHeads], l_of[kDecodeWaves][kDecodeHeads];
     __shared__ int of_wave[2][kDecodeWaves];
@@ -568,8 +567,9 @@ __global__ __launch_bounds__(kSharedThreads, 2) void decode_shared_kernel(Shared
     }
     int before_tail = shared_before(mine_tail, of_wave[1], total_tail);
     // ---- who does what.  Every workgroup takes its share of both kinds, or each does one of them: what ends sooner by an estimate that counts a step of a prefix as kStep and a
-    // tile of a tail as kTile half microseconds.  (With much to do it is the first, where the matrix cores and the memory have work at the same time.)
-    constexpr int kStep = WIDE ? 10 : 4, kTile = 4, kMuch = 8;
+    // tile of a tail as kTile half microseconds (groups of the mean size have wide units or not).  (With much to do it is the first, where the matrix cores and the memory have work at the same time.)
+    const int kStep = d.R * d.group > 32 * p.groups ? 10 : 4;
+    constexpr int kTile = 4, kMuch = 8;
     auto parts = [](int all, int takers) { return (int)(((unsigned)all + (unsigned)takers - 1) / (unsigned)takers); };
     int prefix_takers = grid, tail_takers = grid;
     const bool much = total_prefix >= kMuch * grid;
@@ -727,6 +727,7 @@ __global__ __launch_bounds__(kSharedThreads, 2) void decode_shared_kernel(Shared
             };
             auto narrow_part = [&](auto width) {
                 constexpr int BLOCKS = decltype(width)::value;
+                __syncthreads();      // (others may still read tiles of a wide unit)
                 u4 q[BLOCKS][D / 32];
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b) query(q[b], 16 * b + c);
@@ -744,14 +745,11 @@ __global__ __launch_bounds__(kSharedThreads, 2) void decode_shared_kernel(Shared
                     });
                 }
             };
-            // a unit that fills half of its columns at most computes only those
-            if constexpr (WIDE) {
-                if (columns <= 64) wide_part(std::integral_constant<int, 2>{});
-                else wide_part(std::integral_constant<int, 4>{});
-            } else {
-                if (NB > 1 && columns <= 16) narrow_part(std::integral_constant<int, 1>{});
-                else narrow_part(std::integral_constant<int, NB>{});
-            }
+            // a unit computes no more columns than it has, up to 16, 32, 64
+            if (columns > 64) wide_part(std::integral_constant<int, 4>{});
+            else if (columns > 32) wide_part(std::integral_constant<int, 2>{});
+            else if (columns > 16) narrow_part(std::integral_constant<int, 2>{});
+            else narrow_part(std::integral_constant<int, 1>{});
             if (t0 == 0 && tid == 0) {
                 const long long record = ((long long)begin * d.group / kColumns + g + (part - unit * blocks)) * d.units + unit;
                 p.prefix_records[record] = whole ? int2{-1, 0} : int2{wp, min(wp + (steps - t1 + share_prefix - 1) / share_prefix, prefix_takers - 1)};
@@ -886,7 +884,7 @@ __global__ __launch_bounds__(kSharedThreads, 2) void decode_shared_kernel(Shared
 constexpr int kSharedJoinThreads = 256, kSharedJoinAhead = 4;
 
 template <int D, int GROUPS>
-__global__ __launch_bounds__(kSharedJoinThreads) void decode_shared_join_kernel(SharedParams p, int columns, int grid) {
+__global__ __launch_bounds__(kSharedJoinThreads) void decode_shared_join_kernel(SharedParams p, int grid) {
     constexpr int kAcross = D / 4, kRows = kSharedJoinThreads / (kAcross * GROUPS);
     __shared__ f4 o_of[GROUPS][kRows][kAcross];
     __shared__ f2 sums_of[GROUPS][kRows];
@@ -929,11 +927,11 @@ __global__ __launch_bounds__(kSharedJoinThreads) void decode_shared_join_kernel(
         }
     };
     const bool seen = there && request.w > 0, behind = seen && request.w > request.y, common = seen && request.y > 0;
-    const int at = (r - request.x) * d.group + in_unit, block = (unsigned)at / (unsigned)columns, head_group = in_unit / kDecodeHeads;
+    const int at = (r - request.x) * d.group + in_unit, block = at / kSharedColumns, head_group = in_unit / kDecodeHeads;
     int2 prefix = {0, -1}, tail = {0, -1};
-    if (common) prefix = p.prefix_records[((long long)request.x * d.group / columns + request.z + block) * d.units + unit];
+    if (common) prefix = p.prefix_records[((long long)request.x * d.group / kSharedColumns + request.z + block) * d.units + unit];
     if (behind) tail = p.tail_records[((long long)r * d.units + unit) * d.head_groups + head_group];
-    if (common) add(prefix, p.prefix_parts, p.prefix_sums, columns, at - block * columns, p.rows[0], p.row_sums[0], grid);
+    if (common) add(prefix, p.prefix_parts, p.prefix_sums, kSharedColumns, at - block * kSharedColumns, p.rows[0], p.row_sums[0], grid);
     if (behind) add(tail, p.tail_parts, p.tail_sums, d.heads_kept, in_unit - head_group * kDecodeHeads, p.rows[1], p.row_sums[1], grid * kDecodeWaves);
     if constexpr (GROUPS > 1) {
         o_of[group][of_row][a] = o;
@@ -957,20 +955,20 @@ __global__ __launch_bounds__(kSharedJoinThreads) void decode_shared_join_kernel(
     store_o(d.O + r * d.o_request + head * d.o_head + a * 4 * o_size, d.o_dtype, seen ? o / l : f4{0.f, 0.f, 0.f, 0.f});
 }
 
-// The workspace, in bytes from the front: for the widest units, whichever a call takes.
+// The workspace, in bytes from the front.
 struct SharedWorkspace {
     size_t prefix_sums, tail_parts, tail_sums, rows[2], row_sums[2], requests, prefix_records, tail_records, all;
     SharedWorkspace(const DecodePlan& plan, int R, int H, int groups, int d) {
-        const size_t places = 2 * kSharedGrid, most = (size_t)R * plan.group, columns = most <= 16 ? 16 : most <= 32 ? 32 : kSharedMostColumns, n = (size_t)R * H;
-        size_t at = places * columns * d * 4;
+        const size_t places = 2 * kSharedGrid, n = (size_t)R * H;
+        size_t at = places * kSharedColumns * d * 4;
         auto next = [&](size_t& where, size_t bytes) { where = at; at += (bytes + 15) / 16 * 16; };
-        next(prefix_sums, places * columns * 8);
+        next(prefix_sums, places * kSharedColumns * 8);
         next(tail_parts, kDecodeWaves * places * plan.heads_kept * d * 4);
         next(tail_sums, kDecodeWaves * places * plan.heads_kept * 8);
         for (int i = 0; i < 2; ++i) next(rows[i], n * d * 4);
         for (int i = 0; i < 2; ++i) next(row_sums[i], n * 8);
         next(requests, 16 * (size_t)R);
-        next(prefix_records, 8 * ((size_t)R * plan.group / 16 + groups + 1) * plan.units);
+        next(prefix_records, 8 * ((size_t)R * plan.group / kSharedColumns + groups + 1) * plan.units);
         next(tail_records, 8 * (size_t)R * plan.units * plan.head_groups);
         all = at;
     }
@@ -988,19 +986,14 @@ int shared_plan(const sawattn_kv_cache* cache, int R, int H, int groups, int max
 
 template <int D, bool BF16>
 int launch_shared(const SharedParams& p, int grid, hipStream_t stream) {
-    // As many blocks of 16 columns as the groups fill if they are of one size: a unit computes the ones it has.
-    const int mean = (int)(((long long)p.d.R * p.d.group + p.groups - 1) / p.groups), blocks = mean > 32 ? 8 : mean > 16 ? 2 : 1;
-    const size_t lists = sizeof(int) * (3 * (size_t)p.groups + 1 + p.d.R);
-    if (blocks == 8) hipLaunchKernelGGL((decode_shared_kernel<D, BF16, 8>), dim3(grid), dim3(kSharedThreads), lists, stream, p);
-    else if (blocks == 2) hipLaunchKernelGGL((decode_shared_kernel<D, BF16, 2>), dim3(grid), dim3(kSharedThreads), lists, stream, p);
-    else hipLaunchKernelGGL((decode_shared_kernel<D, BF16, 1>), dim3(grid), dim3(kSharedThreads), lists, stream, p);
+    hipLaunchKernelGGL((decode_shared_kernel<D, BF16>), dim3(grid), dim3(kSharedThreads), sizeof(int) * (3 * (size_t)p.groups + 1 + p.d.R), stream, p);
     const int rc = launched("attn_decode_shared");
     if (rc != SAWATTN_OK) return rc;
     const int rows = p.d.R * p.H;
     constexpr int kAcross = D / 4, kRows4 = kSharedJoinThreads / (4 * kAcross), kRows1 = kSharedJoinThreads / kAcross;
     // (2080 rows of 5 parts 7.9 us with 4, 8.7 with 1; 8192 of 4 17 and 11)
-    if (rows <= 4096) hipLaunchKernelGGL((decode_shared_join_kernel<D, 4>), dim3((rows + kRows4 - 1) / kRows4), dim3(kSharedJoinThreads), 0, stream, p, 16 * blocks, grid);
-    else hipLaunchKernelGGL((decode_shared_join_kernel<D, 1>), dim3((rows + kRows1 - 1) / kRows1), dim3(kSharedJoinThreads), 0, stream, p, 16 * blocks, grid);
+    if (rows <= 4096) hipLaunchKernelGGL((decode_shared_join_kernel<D, 4>), dim3((rows + kRows4 - 1) / kRows4), dim3(kSharedJoinThreads), 0, stream, p, grid);
+    else hipLaunchKernelGGL((decode_shared_join_kernel<D, 1>), dim3((rows + kRows1 - 1) / kRows1), dim3(kSharedJoinThreads), 0, stream, p, grid);
     return launched("attn_decode_shared");
 }
 

@@ -511,7 +511,8 @@ def test_decode_shared_outputs_and_scales(dtype, out, scale):
                                           ([(64 * i, [i, 2 * i, 0]) for i in range(1, 60)], 1, 2, 64), ([(100000, [3, 3])], 1, 1, 128), ([(33, [2])] * 300, 1, 3, 64),
                                           ([(160, [1, 2])] * 1500, 1, 1, 64), ([(0, [20] * 4)] * 3, 8, 4, 128), ([(700, [1] * 5)] * 40, 8, 7, 128),
                                           ([(64, [1] * 64)] * 64, 1, 1, 128), ([(0, [1])] * 4096, 1, 1, 64), ([(32, [5, 9] * 20)] * 3, 2, 33, 128), ([(1500, [700] * 90)], 1, 2, 64),
-                                          ([(0, [1])] * 4094 + [(48, [1, 2])], 1, 40, 128)])
+                                          ([(0, [1])] * 4094 + [(48, [1, 2])], 1, 40, 128),
+                                          ([(1000, [1] * 40), (900, [5, 0]), (1500, [9] * 6), (0, [700]), (1200, [3] * 11)] * 6, 2, 4, 128)])
 def test_decode_shared_sizes(groups, KH, G, d):
     """One step to a workgroup and many, one unit and thousands, groups that a unit holds and groups of many units."""
     case = fill_groups(groups, [], KH, d, 16, "bf16", seed=len(groups))
@@ -867,7 +868,7 @@ def test_built_kernels_have_no_scratch_memory(tmp_path):
     notes = llvm_tool("llvm-readelf", "--notes", device_code(tmp_path))
     found = dict(re.findall(r"\.name:\s+(_ZN7sawattn\d+(?:kv_(?:fork|fork_table|fork_free|fork_few|copy|shared_rows)|decode_shared|decode_shared_join)_kernel\S+)\s+"
                             r"\.private_segment_fixed_size:\s+(\d+)", notes, re.S))
-    assert len(found) == 7 + 12 + 4 and set(found.values()) == {"0"}, found
+    assert len(found) == 7 + 4 + 4 and set(found.values()) == {"0"}, found
 
 
 def test_built_wide_kernels_wait_for_what_they_send_to_lds(tmp_path):
@@ -876,7 +877,7 @@ def test_built_wide_kernels_wait_for_what_they_send_to_lds(tmp_path):
     from .util import device_listing, kernel_bodies
     seen = 0
     for kernel, body in kernel_bodies(device_listing(tmp_path)).items():
-        if not re.search(r"decode_shared_kernel<\d+, (true|false), 8>", kernel):
+        if not re.search(r"decode_shared_kernel<\d+, (true|false)>", kernel):
             continue
         flying, loads, barriers = False, 0, 0
         for text, _ in body:
