@@ -495,7 +495,7 @@ int attn_kv_copy(const sawattn_kv_cache* caches, int layers, const int32_t* copi
  *   table          device, read: int32 [R] rows of max_pages >= 1 entries, table_stride apart; max_pages*page_size below 2^31
  *   group_offsets  device, read: int32 [groups + 1], 1 <= groups <= SAWATTN_MOST_REQUESTS; outside 0 .. R they count as the nearest of these
  *   shared         device, written: int32 [groups], must not overlap the inputs
- * One launch; no workspace.  Stream and errors as attn_fwd.
+ * One launch, two where R*max_pages/groups is more than 131072; no workspace.  Stream and errors as attn_fwd.
  */
 int attn_kv_shared_rows(const int32_t* lengths, int R, const int32_t* table, int64_t table_stride, int max_pages, int page_size,
                         const int32_t* group_offsets, int groups, int32_t* shared, void* hip_stream);

@@ -386,12 +386,14 @@ __global__ __launch_bounds__(kCopyThreads) void kv_copy_kernel(CopyParams p) {
 
 // ---- common rows
 //
-// A workgroup to a group; a thread to a table column, of which it looks at all requests' entries (or a share of them, where there are fewer columns than threads),
-// sixteen on their way at a time.  8 requests of 250 pages 3.9 us, 40 groups of 25 of up to 1024 pages 7, one of 256 requests of 260 pages 13.
-constexpr int kCommonThreads = 1024, kCommonAhead = 16;
+// A workgroup to a group; a thread to a table column and a share of the requests, at whose entries it looks, sixteen on their way at a time.  8 requests of 250 pages 4 us, 40 groups
+// of 25 of up to 1024 pages 7, one of 256 requests of 260 pages 10.  A compute unit reads 14000 entries a microsecond: where groups have more than kCommonSplit of them on average, a
+// first launch writes what the lengths allow and in a second one several workgroups to a group lower that (1000 requests of 512 pages 40 -> 13 us; a launch is 4).
+constexpr int kCommonThreads = 1024, kCommonAhead = 16, kCommonSplit = 1 << 17, kCommonParts = 64;
+enum CommonPass : int { kCommonAll, kCommonLengths, kCommonPages };
 
 __global__ __launch_bounds__(kCommonThreads) void kv_shared_rows_kernel(const int* lengths, const int* table, long long stride, int max_pages, int shift,
-                                                                      const int* offsets, int R, int* shared) {
+                                                                      const int* offsets, int R, int* shared, int pass) {
     __shared__ int least, count, differ;
     __shared__ unsigned short there[SAWATTN_MOST_REQUESTS];      // the requests that hold a row, in any order
     const int tid = threadIdx.x, g = blockIdx.x;
@@ -412,27 +414,37 @@ __global__ __launch_bounds__(kCommonThreads) void kv_shared_rows_kernel(const in
     __syncthreads();
     const int n = count;
     const int pages = n ? min(least >> shift, max_pages) : 0;
-    int across = kCommonThreads;      // columns at a time; the threads that are left over take other requests
-    while (across > 64 && across / 2 >= pages) across /= 2;
-    for (int j0 = 0; j0 < pages; j0 += across) {
-        const int j = j0 + (tid & (across - 1));
-        if (j < pages) {
-            const int page = table[there[0] * stride + j];
-            bool same = true;
-            for (int i0 = 1 + tid / across * kCommonAhead; i0 < n; i0 += kCommonAhead * (kCommonThreads / across)) {
-                int other[kCommonAhead];
+    if (pass != kCommonLengths && n > 1) {
+        const int part = pass == kCommonPages ? (int)((unsigned)pages / gridDim.y) + 1 : pages;
+        const int first = min((int)blockIdx.y * part, pages), last = min(first + part, pages);
+        // (quotients of numbers up to 1024: half of one over the divisor is more than the reciprocal is off by)
+        const int across = min(max(last - first, 1), kCommonThreads);
+        const float one = __builtin_amdgcn_rcpf((float)across);
+        const int shares = (int)((kCommonThreads + 0.5f) * one), share = (int)(((float)tid + 0.5f) * one), column = tid - share * across;
+        for (int j0 = first; j0 < last; j0 += across) {
+            const int j = j0 + column;
+            if (j < last && share < shares) {
+                const int page = table[there[0] * stride + j];
+                bool same = true;
+                for (int i0 = 1 + share * kCommonAhead; i0 < n; i0 += kCommonAhead * shares) {
+                    int other[kCommonAhead];
 #pragma unroll
-                for (int i = 0; i < kCommonAhead; ++i) other[i] = table[there[min(i0 + i, n - 1)] * stride + j];
+                    for (int i = 0; i < kCommonAhead; ++i) other[i] = table[there[min(i0 + i, n - 1)] * stride + j];
 #pragma unroll
-                for (int i = 0; i < kCommonAhead; ++i) same = same && other[i] == page;
+                    for (int i = 0; i < kCommonAhead; ++i) same = same && other[i] == page;
+                }
+                if (!same) atomicMin(&differ, j);
             }
-            if (!same) atomicMin(&differ, j);
+            __syncthreads();
+            if (differ < j0 + across) break;      // (uniform: nobody changes it before the next barrier)
+            __syncthreads();
         }
-        __syncthreads();
-        if (differ < j0 + across) break;      // (uniform: nobody changes it before the next barrier)
-        __syncthreads();
     }
-    if (tid == 0) shared[g] = min(differ, pages) << shift;
+    if (tid == 0) {
+        const int rows = min(differ, pages) << shift;
+        if (pass != kCommonPages) shared[g] = rows;
+        else if (differ < pages) atomicMin(shared + g, rows);
+    }
 }
 
 struct ForkWorkspace {      // bytes, from the front
@@ -574,8 +586,20 @@ int attn_kv_shared_rows(const int32_t* lengths, int R, const int32_t* table, int
     const Range out(shared, 4ull * groups);
     for (const Range& i : {Range(lengths, 4ull * R), Range(table, 4ull * ((unsigned long long)(R - 1) * table_stride + max_pages)), Range(group_offsets, 4ull * (groups + 1))})
         if (out.meets(i)) return fail(SAWATTN_ERR_INVALID_ARG, "attn_kv_shared_rows: an output overlaps an input");
-    hipLaunchKernelGGL(kv_shared_rows_kernel, dim3(groups), dim3(kCommonThreads), 0, static_cast<hipStream_t>(hip_stream), lengths, table, (long long)table_stride,
-                       max_pages, page_shift(page_size), group_offsets, R, shared);
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    auto launch = [&](int parts, CommonPass pass) {
+        hipLaunchKernelGGL(kv_shared_rows_kernel, dim3(groups, parts), dim3(kCommonThreads), 0, stream, lengths, table, (long long)table_stride, max_pages,
+                           page_shift(page_size), group_offsets, R, shared, (int)pass);
+    };
+    const long long each = (long long)R * max_pages / groups;      // entries of a group
+    if (each <= kCommonSplit) {
+        launch(1, kCommonAll);
+    } else {
+        launch(1, kCommonLengths);
+        const int status = launched("attn_kv_shared_rows");
+        if (status != SAWATTN_OK) return status;
+        launch((int)std::min<long long>(each / (kCommonSplit / 8) + 1, kCommonParts), kCommonPages);
+    }
     return launched("attn_kv_shared_rows");
 }
 

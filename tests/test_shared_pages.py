@@ -357,7 +357,8 @@ def test_copy_far_into_a_large_cache():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("sizes,ps,wide", [([1], 16, 1), ([2], 16, 5), ([8], 16, 250), ([3, 0, 7, 1, 0], 32, 70), ([300], 16, 40), ([2, 2, 2], 16, 1024), ([5, 4], 16, 1025),
-                                           ([17, 9], 64, 3000), ([1] * 4096, 16, 3), ([4096], 16, 2)])
+                                           ([17, 9], 64, 3000), ([1] * 4096, 16, 3), ([4096], 16, 2),
+                                           ([1000], 16, 512), ([300, 2], 32, 1500), ([4090, 0, 6], 16, 100), ([1], 16, 140000), ([2, 1], 16, 200000), ([129], 64, 1017), ([100], 16, 65)])
 def test_shared_rows(sizes, ps, wide):
     rng = np.random.default_rng(sum(sizes) + wide)
     R = sum(sizes)
