@@ -786,6 +786,49 @@ def test_a_search_captured():
 
 
 @pytest.mark.gpu
+def test_many_requests_captured():
+    """Forks and common rows that take several launches, captured, replayed with new inputs and with eager work between, against the calls made one by one."""
+    rng = np.random.default_rng(9)
+    R, wide = 1100, 130
+    lengths, source, rows, table, ring, state, ps, pages = fork_case(rng, R, R, 16, 16 * wide - 20)
+    wide = table.shape[1]
+    assert R * wide > 2 ** 17
+    given = {"lengths": up(lengths), "source": up(source), "rows": up(rows), "table": up(table), "ring": up(ring), "state": up(state), "groups": up([0, R])}
+
+    def calls(x, out):
+        fork = binding.attn_kv_fork(x["lengths"], x["source"], x["table"], x["ring"], x["state"], page_size=ps, pages=pages, rows=x["rows"], table_out=out["table"],
+                                    lengths_out=out["lengths"], copies=out["copies"], free_state_out=out["state"], workspace=out["workspace"])
+        binding.attn_kv_shared_rows(x["table"], x["lengths"], x["groups"], page_size=ps, shared=out["shared"])
+        return fork
+
+    def outputs():
+        i32 = {"dtype": torch.int32, "device": "cuda"}
+        return {"table": torch.full((R, wide), POISON, **i32), "lengths": torch.full((R,), POISON, **i32), "copies": torch.full((R, 3), POISON, **i32), "state": torch.full((2,), POISON, **i32),
+                "shared": torch.full((1,), POISON, **i32), "workspace": torch.full((binding.attn_kv_fork_workspace_bytes(R, R, pages),), 0xff, dtype=torch.uint8, device="cuda")}
+    mine, apart = {n: t.clone() for n, t in given.items()}, outputs()
+    calls(mine, outputs())      # (so that everything is loaded)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(mine, apart)
+    for trial in range(6):
+        same = (0, 50, wide, 1, 17, 0)[trial]
+        changed = {n: t.clone() for n, t in given.items()}
+        changed["table"][:, :same] = changed["table"][0, :same]
+        changed["lengths"].copy_(torch.where(changed["lengths"] > 0, 16 * (wide - 1) + 3, 0) if trial % 2 else given["lengths"].roll(trial))
+        changed["source"].copy_(given["source"].roll(7 * trial))
+        for n, t in changed.items():
+            mine[n].copy_(t)
+        for t in apart.values():
+            t.fill_(POISON if t.dtype == torch.int32 else 0xff)
+        graph.replay()
+        want = outputs()
+        calls(changed, want)
+        torch.cuda.synchronize()
+        assert all(torch.equal(apart[n], want[n]) for n in want if n != "workspace") and torch.equal(mine["ring"], changed["ring"]), trial
+        assert want["shared"].tolist() == so.shared_rows(changed["table"].cpu().numpy(), changed["lengths"].tolist(), [0, R], ps), trial
+
+
+@pytest.mark.gpu
 def test_searches_on_streams_of_their_own():
     """Two searches at once on two streams, each with its own workspaces, and calls that are given their stream: the results of one after the other."""
     make = lambda i: Beams([1500, 700 + i], 16, 32, 8, 128, 16, "bf16", seed=3 + i, wide=110)
