@@ -567,7 +567,8 @@ __global__ __launch_bounds__(kSharedThreads, 2) void decode_shared_kernel(Shared
     }
     int before_tail = shared_before(mine_tail, of_wave[1], total_tail);
     // ---- who does what.  Every workgroup takes its share of both kinds, or each does one of them: what ends sooner by an estimate that counts a step of a prefix as kStep and a
-    // tile of a tail as kTile half microseconds (groups of the mean size have wide units or not).  (With much to do it is the first, where the matrix cores and the memory have work at the same time.)
+    // tile of a tail as kTile half microseconds (groups of the mean size have wide units or not; with 7 or 14 for 10, or 3 or 6 for kTile,
+    // 64 requests behind 8192 rows take 42 instead of 41 us and the join 9 instead of 8).  (With much to do it is the first, where the matrix cores and the memory have work at the same time.)
     const int kStep = d.R * d.group > 32 * p.groups ? 10 : 4;
     constexpr int kTile = 4, kMuch = 8;
     auto parts = [](int all, int takers) { return (int)(((unsigned)all + (unsigned)takers - 1) / (unsigned)takers); };
