@@ -3211,7 +3211,7 @@ int attn_fwd_plan(int B, int H, int N, int d, int causal, int scan_order, int in
 }
 
 const char* attn_last_error(void) { return sawattn::g_err; }
-int attn_version(void) { return 220; }
+int attn_version(void) { return 230; }
 const char* sawattn_last_error(void) { return attn_last_error(); }
 int sawattn_version(void) { return attn_version(); }
 
