@@ -54,9 +54,10 @@ struct SharedParams {
     int2* tail_records;
 };
 
-// Two probabilities as sums of two 16-bit numbers each: the first is cut off, the second what is left, rounded (bfloat16) or cut off (binary16).  The second is
-// never zero either, since its product with an infinite value would be no number: bfloat16 takes what is left of a number larger by 2^-20, binary16 at least
-// the smallest number there is, 2^-35 of the reference.
+// Two probabilities as sums of two 16-bit numbers each: the first is cut off, the second what is left, rounded (bfloat16) or cut off (binary16).  Where the
+// first is not zero the second is not either, since its product with an infinite value would be no number: bfloat16 takes what is left of a number larger by
+// 2^-20, binary16 at least the smallest number there is, 2^-35 of the reference.  A binary16 probability below that is cut off, and both numbers are zero: were the second not,
+// thousands of rows without weight would add up to what a row of small values that has all of it cannot stand beside.
 template <bool BF16>
 struct SharedPieces {
     static constexpr int kCount = 2;
@@ -71,7 +72,7 @@ struct SharedPieces {
             constexpr float kMore = 1.f + 0x1p-20f;
             return narrow<true>(__builtin_fmaf(a, kMore, -widen<true>(first, 0)), __builtin_fmaf(b, kMore, -widen<true>(first, 1)));
         } else {
-            return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(fmaxf(a - widen<false>(first, 0), 0x1p-24f), fmaxf(b - widen<false>(first, 1), 0x1p-24f)));
+            return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(fmaxf(a - widen<false>(first, 0), fminf(a, 0x1p-24f)), fmaxf(b - widen<false>(first, 1), fminf(b, 0x1p-24f))));
         }
     }
 };

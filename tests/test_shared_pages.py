@@ -666,6 +666,29 @@ def test_decode_shared_rising_scores(dtype, G):
     check_shared(attend(case, q, 1.0, o_dtype=torch.float32), q, keys, 1.0, lengths, dtype)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [1, 6, 12, 32])      # 4, 24, 48 and 128 columns to a unit: every kind of it
+def test_decode_shared_rows_of_no_weight(dtype, d, G):
+    """One row of small values that has all of the weight, in front of thousands of large ones of one sign whose probabilities are e^-4096 and less: 0 in 32 bits, and
+    0 in what enters the second product.  The result is that row.
+
+    |error| <= |row| * (error of its probability in 16-bit parts, as in check_shared: 2^-20 at binary16, 2^-15 at bfloat16, and what a sum of two parts may be raised by, 2^-35;
+    sums, factors of at most three joins and the quotient: fewer than 16 roundings of 2^-24)."""
+    case = fill_groups([(9008, [700, 20, 5, 40])], [9000], 1, d, 16, dtype, seed=13)
+    cache, table, lengths, offsets, shared, _ = case
+    q = torch.full((5, G, d), 4096.0 / d / 8, dtype=DTYPES[dtype], device="cuda")
+    row = queries(1, 1, d, dtype, seed=14)[0, 0] / 1024
+    cache.k.zero_()
+    cache.v.fill_(60000.0 if dtype == "f16" else 2.0 ** 100)
+    for r in (0, 4):      # all of a group have the first page in common
+        cache.k[int(table[r, 0]), 0, 3], cache.v[int(table[r, 0]), 0, 3] = 8.0, row
+    got = f64(attend(case, q, 1.0, o_dtype=torch.float32))
+    off = np.abs(got - f64(row)) / np.abs(f64(row))
+    assert (off <= (2.0 ** -20 if dtype == "f16" else 2.0 ** -15) + 2.0 ** -35 + 2.0 ** -20).all(), off.max()
+
+
 # ------------------------------------------------------------------------------------------- all of them together
 
 class Beams:
