@@ -513,7 +513,8 @@ int attn_kv_shared_rows(const int32_t* lengths, int R, const int32_t* table, int
  * The result is that of attn_decode, up to rounding: of the probabilities 16 bits (bfloat16) or
  * 22 (binary16, ending at 2^-35 of the largest) enter the second product.  Requests of length 0, values that are infinite and pages that there are not as in
  * attn_decode (a bad page among the shared ones may make O of the whole group NaN; an infinity meets NaN where its probability is less than 2^-35 of the largest).  The result does not depend on timing.
- * Two launches; where R*cache->heads*max_pages*page_size*d are few, up to 12 million or 50 million, those of attn_decode.  Stream and errors as attn_fwd.
+ * Two launches; where R*cache->heads*max_pages*page_size*d are few, up to 12 million or 50 million, or |scale| is below 6.9e-31, those of attn_decode.  Stream and errors
+ * as attn_fwd.
  */
 int attn_decode_shared(const void* Q, int64_t q_request, int64_t q_head, void* O, int64_t o_request, int64_t o_head, int o_dtype,
                        const sawattn_kv_cache* cache, const int32_t* table, int64_t table_stride, int max_pages, const int32_t* lengths,

@@ -34,13 +34,15 @@ constexpr int kSharedColumns = 128;   // of a prefix unit at most
 // need one launch.  The two here take 12 us at least.  32 + 2 x 8 heads of 128, requests x rows in common + own: 4 x 2000 + 100, 35 MB: 14.2 us, attn_decode 12.1; 8 x 2000 + 100, 69 MB: 14.8
 // and 16.9; in one launch (the caches serve most of what is read again) 64 x 500 + 100, 159 MB: 20.7 and 11.3.
 constexpr long long kSharedFew = 48LL << 20, kSharedFewDirect = 192LL << 20;
+// Smaller factors of the scores than this, 0 among them, are attn_decode's kernels': the ones here mask a score by -inf before they multiply it, and divide by the factor.
+constexpr float kSharedLeastFactor = 1e-30f;
 
 struct SharedParams {
     DecodeParams d;           // the query, the cache, the table, as in attn_decode (its workspace is not used)
     const int* offsets;       // [groups + 1]
     const int* shared;        // [groups]
     int groups, H;
-    float c;                  // |scale| * log2(e), 1e-30 at least: the factor of the scores ...
+    float c;                  // |scale| * log2(e), kSharedLeastFactor at least: the factor of the scores ...
     int negative;             // ... and whether the queries change sign
     // workspace
     float* prefix_parts;      // [2 * grid][kSharedColumns][D]
@@ -1046,10 +1048,10 @@ int attn_decode_shared(const void* Q, int64_t q_request, int64_t q_head, void* O
     for (const Range& i : {Range(group_offsets, 4ull * (groups + 1)), Range(shared, 4ull * groups)})
         if (o.meets(i) || scratch.meets(i)) return fail(SAWATTN_ERR_INVALID_ARG, "O and workspace must not overlap what is read");
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if ((double)R * plan.units * p.d.capacity * 4 * d <= (double)(plan.direct ? kSharedFewDirect : kSharedFew))
+    if ((double)R * plan.units * p.d.capacity * 4 * d <= (double)(plan.direct ? kSharedFewDirect : kSharedFew) || std::fabs(p.d.c) < kSharedLeastFactor)
         return run_decode(p.d, plan, H, d, cache->dtype, decode_bytes(plan, d) ? workspace : nullptr, stream);
     p.offsets = group_offsets; p.shared = shared; p.groups = groups; p.H = H;
-    p.c = std::max(std::fabs(p.d.c), 1e-30f); p.negative = scale < 0;
+    p.c = std::fabs(p.d.c); p.negative = scale < 0;
     char* const w = static_cast<char*>(workspace);
     p.prefix_parts = reinterpret_cast<float*>(w); p.prefix_sums = reinterpret_cast<f2*>(w + at.prefix_sums);
     p.tail_parts = reinterpret_cast<float*>(w + at.tail_parts); p.tail_sums = reinterpret_cast<f2*>(w + at.tail_sums);

@@ -689,6 +689,24 @@ def test_decode_shared_rows_of_no_weight(dtype, d, G):
     assert (off <= (2.0 ** -20 if dtype == "f16" else 2.0 ** -15) + 2.0 ** -35 + 2.0 ** -20).all(), off.max()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("G", [1, 12])
+@pytest.mark.parametrize("scale", [0.0, 1e-36, -1e-36, 3e-34])
+def test_decode_shared_scales_next_to_nothing(scale, G):
+    """Scales so small that only products of queries and keys next to the largest numbers of 32 bits make a difference (none at scale 0): as in attn_decode."""
+    d = 64
+    case = fill_groups([(3008, [100, 5, 40, 0, 7, 9]), (160, [3, 8])], [500], 1, d, 16, "bf16", seed=15)
+    cache, table, lengths, offsets, shared, keys = case
+    R = len(lengths)
+    q = torch.zeros(R, G, d, dtype=torch.bfloat16, device="cuda")
+    q[:, :, 5] = 2.0 ** 62
+    cache.k *= 2.0 ** 61      # (a product is up to 2^126)
+    for x in keys[0]:
+        x *= 2.0 ** 61
+    got = attend(case, q, scale, o_dtype=torch.float32)
+    check_shared(got, q, keys, scale, lengths, "bf16")
+
+
 # ------------------------------------------------------------------------------------------- all of them together
 
 class Beams:
