@@ -480,7 +480,7 @@ int attn_kv_fork_workspace_bytes(int R, int N, int pages, size_t* bytes);
  * attn_kv_copy -- copies the first copies[i][2] rows of page copies[i][0] to page copies[i][1], K and V, all heads, in every one of the caches.
  *
  *   caches   host array of `layers` >= 1 structs, read during the call; alike in all but pointers and strides
- *   copies   device, read: int32 [n][3], 1 <= n <= SAWATTN_MOST_REQUESTS, n*heads*page_size below 2^31.  An entry with a page outside
+ *   copies   device, read: int32 [n][3], 1 <= n <= SAWATTN_MOST_REQUESTS, n*heads*page_size below 2^31 - 128.  An entry with a page outside
  *            0 .. pages - 1, or twice the same one, copies nothing; rows count as 0 .. page_size.
  * No page may be written twice, or written and read (the list of attn_kv_fork has no such ones).  One launch for 32 caches; no workspace.  Stream and
  * errors as attn_fwd.

@@ -543,7 +543,8 @@ int attn_kv_copy(const sawattn_kv_cache* caches, int layers, const int32_t* copi
         if (c.pages != one.pages || c.page_size != one.page_size || c.heads != one.heads || c.d != one.d || c.dtype != one.dtype)
             return fail(SAWATTN_ERR_INVALID_ARG, "caches must share pages, page_size, heads, d and dtype");
     }
-    if ((long long)n * one.heads * one.page_size >= (1LL << 31)) return fail(SAWATTN_ERR_INVALID_ARG, "n*heads*page_size must be below 2^31");
+    if ((long long)n * one.heads * one.page_size >= (1LL << 31) - 128)      // (rows are counted in 32 bits, rounded up to pieces of 64 or 128)
+        return fail(SAWATTN_ERR_INVALID_ARG, "n*heads*page_size must be below 2^31 - 128");
     const Range list(copies, 12ull * n);
     auto extent = [](int count, int64_t stride) { return count > 1 ? (unsigned long long)(count - 1) * stride : 0ull; };
     for (int l = 0; l < layers; ++l) {

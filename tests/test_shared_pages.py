@@ -81,6 +81,15 @@ def test_copy_refusals():
     refused(call(caches=ctypes.addressof(big), layers=1), bad, "below 2^31")
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,heads,page_size", [(1, 2 ** 27 - 1, 16), (1, 2 ** 27 - 3, 16)])
+def test_copy_refuses_rows_that_do_not_round_up(n, heads, page_size, d):
+    """n*heads*page_size below 2^31, but not what the pieces count that the rows are dealt out in.  (Heads that all lie in the same place.)"""
+    cache = cache_struct(d=d, heads=heads, page_size=page_size, k_head=0, v_head=0)
+    assert n * heads * page_size < 2 ** 31
+    refused(binding.lib().attn_kv_copy(ctypes.addressof(cache), 1, 0x1000000, n, None), binding.ERR_INVALID_ARG, "below 2^31")
+
+
 def test_shared_rows_refusals():
     L = binding.lib()
     base = dict(lengths=0x100000, R=4, table=0x200000, stride=8, wide=8, ps=16, offsets=0x300000, groups=2, shared=0x400000)
