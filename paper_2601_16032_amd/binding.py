@@ -520,6 +520,8 @@ def attn_kv_fork(lengths, source, table, free_pages, free_state, *, page_size: i
 
 def attn_kv_copy(caches, copies, stream=None):
     """Copies rows of pages as copies[i] = (from, to, rows) says, K and V, all heads, in a KVCache or in all caches of a KVLayers.  Returns without waiting."""
+    if not isinstance(caches, (KVCache, KVLayers)):
+        raise ValueError("caches must be a KVCache, or a KVLayers of several")
     layers = caches.count if isinstance(caches, KVLayers) else 1
     device = caches.device
     rc = (_paged or _paged_module()).kv_copy(caches.ptr, layers, device, copies, _stream_on(device, stream))

@@ -90,6 +90,13 @@ def test_copy_refuses_rows_that_do_not_round_up(n, heads, page_size, d):
     refused(binding.lib().attn_kv_copy(ctypes.addressof(cache), 1, 0x1000000, n, None), binding.ERR_INVALID_ARG, "below 2^31")
 
 
+def test_copy_wants_caches_of_its_own_kinds():
+    """Caches of several layers come as a KVLayers; anything else is refused as such, before a tensor is looked at."""
+    for caches in ([], [1], (object(), object()), None, torch.zeros(3)):
+        with pytest.raises(ValueError, match="KVLayers"):
+            binding.attn_kv_copy(caches, torch.zeros(1, 3, dtype=torch.int32))
+
+
 def test_shared_rows_refusals():
     L = binding.lib()
     base = dict(lengths=0x100000, R=4, table=0x200000, stride=8, wide=8, ps=16, offsets=0x300000, groups=2, shared=0x400000)
