@@ -295,6 +295,25 @@ def test_fork_whatever_the_numbers():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("wide,N", [(1100, 10), (2100, 7), (40, 1030)])
+@pytest.mark.parametrize("room", [30, 20000])
+def test_fork_whatever_the_numbers_of_long_tables(wide, N, room):
+    """The same where three launches share the work (tables of more than 16384 entries in all, or more than 1024 requests)."""
+    big, rng = 2 ** 31 - 1, np.random.default_rng(wide)
+    assert (5 + N) * wide > 16384
+    pages = 5 * wide - 70                                             # the last ones of the last request are outside, as are
+    table = np.arange(5 * wide).reshape(5, wide)
+    table[2, 1], table[4, 0], table[0, 3], table[3, wide - 1], table[1, 30], table[0, 17] = big, -big - 1, pages, -1, pages + 5, 7
+    ring = np.arange(room) - 10
+    lengths = np.array([big, -3, 16 * wide - 5, 16 * wide, 20 * 16])
+    source = np.resize([0, 0, 1, 2, 2, 4, 3, 3, 77, -5], N)
+    rows = np.resize([big, 33, 5, 16 * wide - 7, 17, -4, 16 * wide - 9, 0, 3, 3, big, 16 * 20 + 1], N)
+    for first, free in ((3, 8), (-1, 50000), (room, 8), (big, big), (2, -4), (room - 1, 2)):
+        check_fork(lengths, source, rows, table, ring, [first, free], 16, pages, stride=5)
+        check_fork(lengths, rng.permutation(source), None, table, ring, [first, free], 16, pages)
+
+
+@pytest.mark.gpu
 def test_forks_and_appends_lose_no_page():
     """Some dozen steps of a server that branches, cuts short, ends and appends: pages held and pages free are all pages, every page once, and a page that
     is written on is one request's."""
