@@ -63,8 +63,9 @@ struct SharedParams {
 template <bool BF16>
 struct SharedPieces {
     static constexpr int kCount = 2;
-    // A maximum is raised for scores by more than kSlack (in powers of two) above it; binary16 probabilities are scaled by 2^kShift, up to 2^15 with the slack.
-    static constexpr float kSlack = BF16 ? kRescaleSlack : 4.f, kShift = BF16 ? 0.f : 11.f;
+    // A maximum is raised for scores by more than kSlack (in powers of two) above it; probabilities are scaled by 2^kShift: binary16 ones come up to 2^15 with the slack, bfloat16
+    // ones up to 1, so that no value grows by its weight (values next to the largest number overflowed).
+    static constexpr float kSlack = BF16 ? kRescaleSlack : 4.f, kShift = BF16 ? -kRescaleSlack : 11.f;
     static __device__ __forceinline__ unsigned first(float a, float b) {
         if constexpr (BF16) return __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
         else return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(a, b));
@@ -115,7 +116,7 @@ struct RowsState {
             for (int j = 0; j < D / 16; ++j) o[b][j] = f4{0.f, 0.f, 0.f, 0.f};
             l[b] = 0.f;
             limit[b] = -INFINITY;
-            shift[b] = Pieces::kShift;
+            shift[b] = 0.f;      // (any number will do: there is no score yet)
         }
     }
     __device__ __forceinline__ float reference(int b) const { return limit[b] == -INFINITY ? -INFINITY : -shift[b]; }
@@ -286,7 +287,7 @@ struct WideState {
             for (int j = 0; j < D / 16; ++j) o[b][j] = f4{0.f, 0.f, 0.f, 0.f};
             l[b] = 0.f;
             limit[b] = -INFINITY;
-            shift[b] = Pieces::kShift;
+            shift[b] = 0.f;      // (any number will do: there is no score yet)
         }
     }
     __device__ __forceinline__ float reference(int b) const { return limit[b] == -INFINITY ? -INFINITY : -shift[b]; }

@@ -742,6 +742,33 @@ def test_decode_shared_scales_next_to_nothing(scale, G):
     check_shared(got, q, keys, scale, lengths, "bf16")
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [1, 12, 24, 40])      # 2, 24, 48 and 80 columns to a unit: every kind of it
+def test_decode_shared_values_next_to_the_largest(G, d):
+    """bfloat16 values that may not grow by the weight of their rows: of 100000 rows some have scores above those of the rows in front of them, by less than what a
+    reference is raised for, and values next to the largest there are.  Each has an element to itself, where O is their value times their probability.
+
+    |error| <= relative error of a probability, as in check_shared: 2^-15 for its parts, 2^-19 for exp2, one addition for every 32 rows and joining; the
+    scores are exact."""
+    n, own, most = 100032, 4000, 1.5 * 2.0 ** 126
+    case = fill_groups([(n, [own, 0])], [n], 1, d, 64, "bf16", seed=16)
+    cache, table, lengths, offsets, shared, _ = case
+    q = torch.zeros(3, G, d, dtype=torch.bfloat16, device="cuda")
+    q[:, :, 3] = 1.0
+    cache.k.zero_()
+    cache.v.zero_()
+    heavy = [(0, n * i // 20 + 77, 8 + i) for i in range(20)] + [(0, n + 2000 + 300 * i, 30 + i) for i in range(3)] + [(2, n * i // 20 + 77, 8 + i) for i in range(20)]
+    for r, at, element in heavy:
+        cache.k[int(table[r, at // 64]), 0, at % 64, 3], cache.v[int(table[r, at // 64]), 0, at % 64, element] = 56.0, most
+    got = f64(attend(case, q, math.log(2.0) / 8, o_dtype=torch.float32))      # a key of 56 in element 3: a score of 7 in powers of two
+    for r in range(3):
+        seen = {element for s, at, element in heavy if (s, r) in ((0, 0), (0, 1), (2, 2)) and at < lengths[r]}
+        want = np.zeros(d)
+        want[sorted(seen)] = most * 128.0 / (128 * len(seen) + lengths[r] - len(seen))
+        assert (np.abs(got[r] - want) <= (2.0 ** -15 + 2.0 ** -19 + (n / 32 + 64) * 2.0 ** -23) * want).all(), (r, got[r, 0], want)
+
+
 # ------------------------------------------------------------------------------------------- all of them together
 
 class Beams:
