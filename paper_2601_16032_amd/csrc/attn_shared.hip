@@ -80,6 +80,10 @@ struct SharedPieces {
     }
 };
 
+// A column's new reference, of a raw score.  Scores below all numbers (of keys of the lowest value, as masks have them) leave a finite one: a difference from it is one, and their
+// probabilities are 0.
+__device__ __forceinline__ float shared_maximum(float raw, float factor) { return fmaxf(raw * factor, -0x1.fffffep127f); }
+
 // 32 rows in a wavefront's registers, as operands of both products.
 template <int D>
 struct RowsTile {
@@ -183,7 +187,7 @@ struct RowsState {
             for (int b = 0; b < NB; ++b) {
                 const float raw = head_max(most[b]);
                 if (raw > limit[b]) {      // (all four lanes of a column alike)
-                    const float M = raw * factor, fade = limit[b] == -INFINITY ? 1.f : fast_exp2(Pieces::kShift - shift[b] - M);
+                    const float M = shared_maximum(raw, factor), fade = limit[b] == -INFINITY ? 1.f : fast_exp2(Pieces::kShift - shift[b] - M);
                     limit[b] = score_limit(raw, M, factor, Pieces::kSlack);
                     shift[b] = Pieces::kShift - M;
                     l[b] *= fade;
@@ -383,7 +387,7 @@ struct WideState {
             for (int b = 0; b < 2; ++b) {
                 const float t = head_max(most[b]);
                 if (t > limit[b]) {      // (all four lanes of a column alike)
-                    const float M = t * c, fade = limit[b] == -INFINITY ? 1.f : fast_exp2(Pieces::kShift - shift[b] - M);
+                    const float M = shared_maximum(t, c), fade = limit[b] == -INFINITY ? 1.f : fast_exp2(Pieces::kShift - shift[b] - M);
                     limit[b] = score_limit(t, M, c, Pieces::kSlack);
                     shift[b] = Pieces::kShift - M;
                     l[b] *= fade;

@@ -769,6 +769,26 @@ def test_decode_shared_values_next_to_the_largest(G, d):
         assert (np.abs(got[r] - want) <= (2.0 ** -15 + 2.0 ** -19 + (n / 32 + 64) * 2.0 ** -23) * want).all(), (r, got[r, 0], want)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [1, 6, 12, 32])
+def test_decode_shared_keys_of_the_lowest_value(G, d):
+    """Rows masked by the lowest number there is in their keys, whole tiles and units of them, at a scale at which their scores are no numbers of 32 bits: they have no weight."""
+    n, hidden = 5008, 3000
+    case = fill_groups([(n, [700, 20, 5, 400])], [6000], 1, d, 16, "bf16", seed=17)
+    cache, table, lengths, offsets, shared, keys = case
+    q = queries(5, G, d, "bf16", seed=18) / 8
+    q[:, :, 3] = 1.0
+    lowest = torch.finfo(torch.bfloat16).min
+    for r, low, high in ((0, 0, hidden), (0, n, n + 500), (3, n, n + 400), (4, 700, 6000 - 100)):
+        for at in range(low, high):
+            cache.k[int(table[r, at // 16]), 0, at % 16] = 0.0
+            cache.k[int(table[r, at // 16]), 0, at % 16, 3] = lowest
+    seen = [np.r_[hidden:n, n + 500:n + 700], np.r_[hidden:n + 20], np.r_[hidden:n + 5], np.r_[hidden:n], np.r_[0:700, 5900:6000]]
+    kept = [[x[torch.as_tensor(rows, device=x.device)] for x, rows in zip(side, seen)] for side in keys]
+    check_shared(attend(case, q, 1.0, o_dtype=torch.float32), q, kept, 1.0, [len(rows) for rows in seen], "bf16")
+
+
 # ------------------------------------------------------------------------------------------- all of them together
 
 class Beams:
