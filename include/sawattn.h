@@ -522,7 +522,8 @@ int attn_decode_shared(const void* Q, int64_t q_request, int64_t q_head, void* O
                        size_t workspace_bytes, void* hip_stream);
 
 /* attn_decode_shared_workspace_bytes -- the workspace attn_decode_shared needs for R requests of H heads in `groups` groups: 2 d R H floats and at most some
- * 110 MiB, or what attn_decode needs.  The same workspace does for every call of as many requests and groups or fewer.  Launches nothing. */
+ * 110 MiB, or what attn_decode needs.  The same workspace does for every call of as many requests and groups or fewer, with tables as wide or narrower.  Launches
+ * nothing. */
 int attn_decode_shared_workspace_bytes(const sawattn_kv_cache* cache, int R, int H, int groups, int max_pages, size_t* bytes);
 
 /* Text of the last error raised on the calling thread ("" if none).  Static storage, never NULL. */

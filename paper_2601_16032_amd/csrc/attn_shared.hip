@@ -9,22 +9,31 @@
 // (below) for each of them per 4 d bytes: from 64 columns on it is the matrix cores' and the vector units' time that counts.
 //
 // Who does what.  The steps (128 rows) of all prefix units, one behind the other, are dealt out evenly over workgroups, and the tiles (32 rows) of all tail
-// units, the other way round, over wavefronts.  With much to do every workgroup takes its share of both, and of the two workgroups of a compute unit
-// one begins with prefixes and one with tails, so that one computes while the other waits for memory (256 requests behind 32768 rows, 32 + 2 x 8 heads of 128,
-// tails up to 2000: 250 us; prefixes alone 190, tails alone 105).  With little to do a workgroup takes one kind only, where that ends sooner: what
-// counts then are the steps from one address to the next, a microsecond each.  Of each unit that a workgroup ends, begins or goes on with it leaves
-// (m, l, o) in the workspace, and a second kernel joins for every row of O what belongs to it.
+// units, the other way round, over wavefronts.
+//   Much to do: every workgroup takes its share of both, and of the two workgroups of a compute unit one begins with prefixes and one with tails, so that one
+//   computes while the other waits for memory.
+//   Little to do: a workgroup takes one kind only, where that ends sooner; what counts then are the steps from one address to the next, a microsecond each.
+// Of each unit that a workgroup ends, begins or goes on with it leaves (m, l, o) in the workspace, and a second kernel joins for every row of O what belongs to it.
+// (The lists of groups and requests lie in LDS beside the tiles.  At d = 128 two workgroups fit on a compute unit up to 3 groups + requests of about 3900, then
+// one: the second half of the grid begins when the first has ended.)
 //
-// Products run on 16x16x32 MFMAs, transposed: S^T = K Q^T, O^T = V^T P^T.  Up to 32 columns (RowsState) and tails: rows from memory straight into the operands' registers.  More:
-// tiles of 64 rows through LDS that the four wavefronts share, 32 columns each (WideState); 32 columns at a time, 256 requests of 4 heads to a key head behind 32768 rows take 242 us
-// instead of 190 (64 behind 8192 31 and 30; tails left out).  Which it is goes by the unit, so groups of any sizes stand in one call: 256 requests behind 16384 rows and 256 of their own 311 us, 522 with
-// units as wide as the groups' mean; kernels of their own for calls of 16 or 32 columns at most gain 1 to 2 %.
+// Products run on 16x16x32 MFMAs, transposed: S^T = K Q^T, O^T = V^T P^T.
+//   Up to 32 columns (RowsState), and tails: rows from memory straight into the operands' registers.
+//   More: tiles of 64 rows through LDS that the four wavefronts share, 32 columns each (WideState).
+// Which it is goes by the unit, so groups of any sizes stand in one call.
 //
 // The probabilities enter the second product as sums of two 16-bit numbers (SharedPieces), 16 bits of them: one would be off by as much as the
-// rounding of O to 16 bits, three, as in attn_decode, would take a third more of the matrix cores.  256 requests behind 32768 rows, with their tails, run at 0.88 PFLOP/s of MFMAs, 40 % of the rate at 2.1 GHz,
-// which is the clock that the chip then holds; MFMA phases have precedence (210 -> 200 us without the tails).
-// Without their tails they take 190 us, 1.08 PFLOP/s; a large product reaches 1.28.  A pipeline in which the exponentials of 32 rows stand between the MFMAs of the rows before and
-// behind them was no faster (209 us; 178 with nothing but its MFMAs and what feeds them).
+// rounding of O to 16 bits, three, as in attn_decode, would take a third more of the matrix cores.  MFMA phases have precedence over other wavefronts' work.
+//
+// Measured, 32 + 2 x 8 heads of 128, us:
+//   256 requests behind 32768 rows, tails up to 2000    256 (prefixes alone 190, tails alone 105): 0.87 PFLOP/s of MFMAs, 40 % of the rate at the 2.1 GHz that the chip
+//                                                       then holds; prefixes alone 1.08, a large product 1.28
+//   their prefixes, 32 columns at a time                242 instead of 190 (64 requests behind 8192 rows: 31 and 30)
+//   their prefixes, without precedence                  210, with it 200 (before other steps that led to 190)
+//   their prefixes, exponentials of 32 rows between the MFMAs of those before and behind them   209 (178 with nothing but its MFMAs and what feeds them)
+//   256 requests behind 16384 rows and 256 of their own   311; 522 with units as wide as the groups' mean
+//   kernels of their own for calls of 16 or 32 columns at most   1 to 2 % less
+//   4096 requests, 1024 groups of 4 behind 1024 rows, 8 + 2 x 2 heads   436 (attn_decode 713); 960 in 240 groups 80 (168)
 namespace sawattn {
 
 constexpr int kSharedThreads = 64 * kDecodeWaves;
