@@ -92,6 +92,10 @@ struct SharedPieces {
 // A column's new reference, of a raw score.  Scores below all numbers (of keys of the lowest value, as masks have them) leave a finite one: a difference from it is one, and their
 // probabilities are 0.
 __device__ __forceinline__ float shared_maximum(float raw, float factor) { return fmaxf(raw * factor, -0x1.fffffep127f); }
+// Exponents are worked out in one step, raw score * factor + shift.  The product in it is not rounded, the one in the shift was, so that all rows' exponents are off by up to half of the reference's
+// last bit.  That drops out of the quotient unless it is large: the best row's weight would be infinite, or 0.  Where a reference is beyond this number (last bit 2^-3), the scores are scaled and
+// rounded first.
+constexpr float kSharedFar = 0x1p20f;
 
 // 32 rows in a wavefront's registers, as operands of both products.
 template <int D>
@@ -196,14 +200,24 @@ struct RowsState {
             for (int b = 0; b < NB; ++b) {
                 const float raw = head_max(most[b]);
                 if (raw > limit[b]) {      // (all four lanes of a column alike)
-                    const float M = shared_maximum(raw, factor), fade = limit[b] == -INFINITY ? 1.f : fast_exp2(Pieces::kShift - shift[b] - M);
+                    const float M = shared_maximum(raw, factor), next = Pieces::kShift - M, fade = limit[b] == -INFINITY ? 1.f : fast_exp2(next - shift[b]);
                     limit[b] = score_limit(raw, M, factor, Pieces::kSlack);
-                    shift[b] = Pieces::kShift - M;
+                    shift[b] = next;
                     l[b] *= fade;
 #pragma unroll
                     for (int j = 0; j < D / 16; ++j) o[b][j] *= fade;
                 }
             }
+        }
+        bool far = false;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) far = far || fabsf(shift[b]) > kSharedFar;
+        if (__any(far)) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) s[b][half] *= factor;
+            factor = 1.f;
         }
         u4 piece[NB][Pieces::kCount];
 #pragma unroll
@@ -396,14 +410,23 @@ struct WideState {
             for (int b = 0; b < 2; ++b) {
                 const float t = head_max(most[b]);
                 if (t > limit[b]) {      // (all four lanes of a column alike)
-                    const float M = shared_maximum(t, c), fade = limit[b] == -INFINITY ? 1.f : fast_exp2(Pieces::kShift - shift[b] - M);
+                    const float M = shared_maximum(t, c), next = Pieces::kShift - M, fade = limit[b] == -INFINITY ? 1.f : fast_exp2(next - shift[b]);
                     limit[b] = score_limit(t, M, c, Pieces::kSlack);
-                    shift[b] = Pieces::kShift - M;
+                    shift[b] = next;
                     l[b] *= fade;
 #pragma unroll
                     for (int j = 0; j < D / 16; ++j) o[b][j] *= fade;
                 }
             }
+        }
+        if (__any(fabsf(shift[0]) > kSharedFar || fabsf(shift[1]) > kSharedFar)) {
+#pragma unroll
+            for (int sub = 0; sub < SUBS; ++sub)
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) s[sub][b][half] *= c;
+            c = 1.f;
         }
         __builtin_amdgcn_s_setprio(0);
         u4 piece[SUBS][2][Pieces::kCount];

@@ -789,6 +789,57 @@ def test_decode_shared_keys_of_the_lowest_value(G, d):
     check_shared(attend(case, q, 1.0, o_dtype=torch.float32), q, kept, 1.0, [len(rows) for rows in seen], "bf16")
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [0.125, 0.0884, 0.7, -0.31])
+@pytest.mark.parametrize("d,G", [(64, 1), (128, 6), (64, 12), (128, 32)])
+def test_decode_shared_keys_of_the_lowest_value_at_other_scales(d, G, scale):
+    """The same where the masked rows' scores are numbers, of which the last bit is more than any exponent: they have no weight beside others, and all of it, alike, in a request
+    that sees nothing else."""
+    n, hidden = 5008, 3000
+    case = fill_groups([(n, [700, 20, 5, 400])], [6000, 4000], 1, d, 16, "bf16", seed=19)
+    cache, table, lengths, offsets, shared, keys = case
+    q = queries(6, G, d, "bf16", seed=20)
+    q[:, :, 3] = (1.0 + torch.arange(G, device="cuda") / 64).bfloat16() * 0.6
+    masked = torch.finfo(torch.bfloat16).min * (1 if scale > 0 else -1)
+    for r, low, high in ((0, 0, hidden), (0, n, n + 500), (3, n, n + 400), (4, 700, 6000 - 100), (5, 0, 4000)):
+        for at in range(low, high):
+            cache.k[int(table[r, at // 16]), 0, at % 16] = 0.0
+            cache.k[int(table[r, at // 16]), 0, at % 16, 3] = masked
+    seen = [np.r_[hidden:n, n + 500:n + 700], np.r_[hidden:n + 20], np.r_[hidden:n + 5], np.r_[hidden:n], np.r_[0:700, 5900:6000], np.r_[0:4000]]
+    kept = [[x[torch.as_tensor(rows, device=x.device)] for x, rows in zip(side, seen)] for side in keys]
+    kept[0][5] = torch.zeros_like(kept[0][5])      # rows of the same score, whatever it is
+    check_shared(attend(case, q, scale, o_dtype=torch.float32), q, kept, scale, [len(rows) for rows in seen], "bf16")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("scale", [1.0, 0.3, 11.0, -0.7])
+@pytest.mark.parametrize("d,G", [(64, 1), (128, 6), (64, 12), (128, 32)])
+def test_decode_shared_scores_beyond_all_exponents(dtype, scale, d, G):
+    """Scores of two sizes, both so large that the last bit of a scaled one is more than any exponent.  The rows of the larger have all of the weight and share it, so O is the
+    mean of their values.  |error| as in check_shared, without that of the scores, which are alike."""
+    n = 5008
+    case = fill_groups([(n, [700, 20, 5, 400])], [6000], 1, d, 16, dtype, seed=21)
+    cache, table, lengths, offsets, shared, keys = case
+    q = torch.zeros(5, G, d, dtype=DTYPES[dtype], device="cuda")
+    q[:, :, 3] = 24576.0 if dtype == "f16" else 3.0 * 2.0 ** 55
+    more, less = (27648.0, 26624.0) if dtype == "f16" else (27.0 * 2.0 ** 55, 26.0 * 2.0 ** 55)
+    rng, large = np.random.default_rng(1), []
+    for r in range(5):
+        which = rng.random(lengths[r]) < 0.3
+        which[:200] = False
+        if 0 < r < 4:
+            which[:n] = large[0][:n]
+        large.append(which)
+        at = torch.arange(0 if r in (0, 4) else n, lengths[r], device="cuda")
+        cache.k[table[r, at // 16].long(), 0, at % 16, 3] = torch.tensor(np.where(which, more, less)[at.cpu()], device="cuda").to(q.dtype)
+    got = f64(attend(case, q, scale, o_dtype=torch.float32))
+    for r in range(5):
+        v = f64(keys[1][r])[large[r] if scale > 0 else ~large[r], 0]
+        bound = (2.0 ** -15 if dtype == "bf16" else 2.0 ** -20) + 2.0 ** -19 + (n / 32 + 64) * 2.0 ** -23
+        assert (np.abs(got[r] - v.mean(0)) <= 2 * bound * np.abs(v).mean(0)).all(), (r, got[r, 0, :4], v.mean(0)[:4])
+
+
 # ------------------------------------------------------------------------------------------- all of them together
 
 class Beams:
